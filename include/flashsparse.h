@@ -347,6 +347,109 @@ fs_status fs_attention(const fs_format *fmt,
                        void *d_work, size_t work_bytes, void *stream);
 
 /*
+ * A learned bias of the scores by relative position.  The entry of row i and column j of A has the relative position
+ * j - i - shift, clamped to [-reach, reach]; d_bucket names the bucket of each, and head h adds d_table[h * ld + bucket].
+ *   d_table   : biases in the element type, 2-byte aligned; ld >= n_buckets elements from a head to the next (0: all heads share one)
+ *   d_bucket  : 2 * reach + 1 bytes, 4-byte aligned, the bucket of position r at [r + reach]; a bucket above n_buckets - 1
+ *               counts as that one
+ *   n_buckets : 1 .. 128;  reach : 0 .. 1024
+ *   shift     : |shift| < 2^31; the position of row 0 where the rows of A are the last ones of a sequence
+ * A bias of minus infinity takes its entries out; a row of which nothing is left counts as one without entries.
+ */
+typedef struct fs_bucket_bias {
+    const void *d_table;
+    int64_t ld;
+    const uint8_t *d_bucket;
+    int32_t n_buckets, reach;
+    int64_t shift;
+} fs_bucket_bias;
+
+/*
+ * Dropout: an entry is kept where the first word of Threefry-2x32 with 13 rounds at the counter (row, column) is at least
+ * floor(p * 2^32), and multiplied with 1 / (1 - p); the others become zero.  The key of head h is the same generator with 20
+ * rounds at the counter (h, 0), under the key that it yields for the counter `step` under the key `seed` (low word first).
+ * The mask is not stored: the same state draws the same one in every call, whatever the layout.
+ *   p       : in [0, 1); 0 draws nothing
+ *   d_state : two int64 on the device, seed and step, 8-byte aligned; read when the kernels run, so that a program advances the step between
+ *             the replays of a captured graph
+ */
+typedef struct fs_dropout {
+    double p;
+    const int64_t *d_state;
+} fs_dropout;
+
+/* A dense matrix per head: element (row, column) of head h is at d[row * ld + h * head + column] (strides in elements). */
+typedef struct fs_head_matrix {
+    void *d;
+    int64_t ld, head;
+} fs_head_matrix;
+
+/*
+ * The bias on value arrays, the step between fs_sddmm and fs_edge_softmax:
+ *   out[p] = scale * in[p] + the bias of entry p,
+ * for `heads` arrays of V*nvec elements in the vals_blk layout, one behind the other.  fp32 arithmetic, one rounding;
+ * positions outside the pattern get +0.0.  d_out_blk may be d_in_blk.  2-byte aligned arrays; scale is finite; heads >= 0.
+ * fs_edge_bias_backward: the gradient of the table from the gradient g of out,
+ *   grad[h * n_buckets + k] = sum of g over the entries of bucket k   (heads * n_buckets elements, rounded once; the bias's
+ *   table is not read, its ld not looked at).  The gradient of `in` is scale * g.  d_work: fs_edge_bias_backward_workspace_bytes, 16-byte aligned.
+ * Both are asynchronous on `stream` and deterministic (no atomics between wavefronts, sums in a fixed order).
+ */
+fs_status fs_edge_bias(const fs_format *fmt, int32_t heads, const void *d_in_blk, float scale, const fs_bucket_bias *bias,
+                       void *d_out_blk, void *stream);
+fs_status fs_edge_bias_backward_workspace_bytes(const fs_format *fmt, int32_t heads, int32_t n_buckets, size_t *work_bytes);
+fs_status fs_edge_bias_backward(const fs_format *fmt, int32_t heads, const void *d_g_blk, const fs_bucket_bias *bias,
+                                void *d_table_grad, void *d_work, size_t work_bytes, void *stream);
+
+/*
+ * Dropout on value arrays, the step between fs_edge_softmax and fs_spmm, and its own gradient:
+ *   out[p] = in[p] / (1 - p) where the entry is kept, else +0.0
+ * for `heads` arrays of V*nvec elements in the vals_blk layout.  Positions outside the pattern get +0.0.  d_out_blk may be d_in_blk.
+ */
+fs_status fs_edge_dropout(const fs_format *fmt, int32_t heads, const void *d_in_blk, const fs_dropout *drop, void *d_out_blk,
+                          void *stream);
+
+/*
+ * fs_attention as it is trained: for every query head h, with g = h / (heads / kv_heads) the head of keys and values it reads,
+ *   s = scale * (X_h * Y_g^T) + bias_h at the stored positions of A,  P = softmax_rows(s),
+ *   out_h = dropout(P) * H_g,   lse_h = log of the row sums of exp(s).
+ *   X : M x d, out : M x N for each of `heads`;  Y : K x d, H : K x N for each of kv_heads, which divides heads
+ *   d % 8 == 0, N % 8 == 0, both at most 128; leading dimensions and head strides % 8 == 0, pointers 16-byte aligned
+ *   bias, drop : NULL for none (the pass of serving is this call without dropout)
+ *   d_lse : heads x M floats, 4-byte aligned, or NULL; a row without entries gets zeros and minus infinity
+ *   d_work : fs_attention_forward_workspace_bytes, 16-byte aligned (may be NULL when that size is 0)
+ * Scores and probabilities stay in registers in fp32; probabilities are rounded to the element type relative to the running row
+ * maximum for the product with H.  M and K below 2^24; a head of X, Y and H spans less than 4 GiB, a row pitch is below
+ * 2^24 bytes (else FS_ERR_UNSUPPORTED).  As in fs_spmm, inputs are taken to be finite: an infinity or NaN in a row of H reaches all
+ * rows of the windows that reference it.  Asynchronous on `stream`; deterministic.
+ */
+fs_status fs_attention_forward_workspace_bytes(const fs_format *fmt, int32_t heads, int64_t N, size_t *work_bytes);
+fs_status fs_attention_forward(const fs_format *fmt, int32_t heads, int32_t kv_heads, int64_t d, int64_t N, float scale,
+                               const fs_head_matrix *X, const fs_head_matrix *Y, const fs_head_matrix *H,
+                               const fs_bucket_bias *bias, const fs_dropout *drop,
+                               const fs_head_matrix *out, float *d_lse, void *d_work, size_t work_bytes, void *stream);
+
+/*
+ * The gradients of fs_attention_forward.  With G the gradient of out, P = exp(s - lse) and Z the dropout's factors,
+ *   D = row sums of G * out,  dS = P * (Z * (G H^T) - D) at the stored positions,
+ *   dX = scale * dS * Y,  dY = scale * dS^T * X,  dH = (Z * P)^T * G,  dtable[h][k] = sum of dS over bucket k,
+ * dY and dH summed over the query heads that share them.  Two passes: by rows over fmt (dX, dtable) and by columns over
+ * fmt_t, the format of A^T (fs_csr_transpose, fs_convert).  Scores are computed again from X and Y; dS and Z * P are rounded
+ * to the element type for the products (fp16: loss scaling keeps dS out of its subnormal range).
+ *   X, Y, H, bias, drop, scale : as in the forward call, whose out and lse these are;  G : M x N for each of `heads`
+ *   dX, dY, dH : written whole (zeros where nothing is stored), and overlap nothing that is read
+ *   d_table_grad : heads * n_buckets elements in the element type, 2-byte aligned, or NULL
+ *   d_work : fs_attention_backward_workspace_bytes, 16-byte aligned; n_buckets there: the bias's, 0 where no gradient of it is asked for
+ * fmt_t is checked for its sizes and its type.  Other limits as for the forward call.  Asynchronous on `stream`; deterministic.
+ */
+fs_status fs_attention_backward_workspace_bytes(const fs_format *fmt, const fs_format *fmt_t, int32_t heads, int32_t kv_heads, int64_t d,
+                                                int64_t N, int32_t n_buckets, size_t *work_bytes);
+fs_status fs_attention_backward(const fs_format *fmt, const fs_format *fmt_t, int32_t heads, int32_t kv_heads, int64_t d, int64_t N,
+                                float scale, const fs_head_matrix *X, const fs_head_matrix *Y, const fs_head_matrix *H,
+                                const fs_bucket_bias *bias, const fs_dropout *drop, const fs_head_matrix *out, const float *d_lse,
+                                const fs_head_matrix *G, const fs_head_matrix *dX, const fs_head_matrix *dY, const fs_head_matrix *dH,
+                                void *d_table_grad, void *d_work, size_t work_bytes, void *stream);
+
+/*
  * Reorder a value array from the vals_blk layout to CSR order:
  * d_out_csr[p] = d_blk[csr_to_slot[p]] for p in [0, nnz).  Asynchronous.
  */

@@ -51,6 +51,19 @@ class _FsFormatStruct(ctypes.Structure):
     ]
 
 
+class _FsBucketBiasStruct(ctypes.Structure):
+    _fields_ = [("d_table", ctypes.c_void_p), ("ld", ctypes.c_int64), ("d_bucket", ctypes.c_void_p), ("n_buckets", ctypes.c_int32),
+                ("reach", ctypes.c_int32), ("shift", ctypes.c_int64)]
+
+
+class _FsDropoutStruct(ctypes.Structure):
+    _fields_ = [("p", ctypes.c_double), ("d_state", ctypes.c_void_p)]
+
+
+class _FsHeadMatrix(ctypes.Structure):
+    _fields_ = [("d", ctypes.c_void_p), ("ld", ctypes.c_int64), ("head", ctypes.c_int64)]
+
+
 def library_path() -> str:
     return _LIB_PATH
 
@@ -105,6 +118,24 @@ def load_library():
     lib.fs_edge_softmax.argtypes = [fmtp, vp, vp, ctypes.c_float, vp, sz, vp]
     lib.fs_edge_softmax_backward.restype = ctypes.c_int
     lib.fs_edge_softmax_backward.argtypes = [fmtp, vp, vp, ctypes.c_float, vp, vp, sz, vp]
+    mp, biasp, dropp = ctypes.POINTER(_FsHeadMatrix), ctypes.POINTER(_FsBucketBiasStruct), ctypes.POINTER(_FsDropoutStruct)
+    lib.fs_edge_bias.restype = ctypes.c_int
+    lib.fs_edge_bias.argtypes = [fmtp, i32, vp, ctypes.c_float, biasp, vp, vp]
+    lib.fs_edge_bias_backward_workspace_bytes.restype = ctypes.c_int
+    lib.fs_edge_bias_backward_workspace_bytes.argtypes = [fmtp, i32, i32, szp]
+    lib.fs_edge_bias_backward.restype = ctypes.c_int
+    lib.fs_edge_bias_backward.argtypes = [fmtp, i32, vp, biasp, vp, vp, sz, vp]
+    lib.fs_edge_dropout.restype = ctypes.c_int
+    lib.fs_edge_dropout.argtypes = [fmtp, i32, vp, dropp, vp, vp]
+    lib.fs_attention_forward_workspace_bytes.restype = ctypes.c_int
+    lib.fs_attention_forward_workspace_bytes.argtypes = [fmtp, i32, i64, szp]
+    lib.fs_attention_forward.restype = ctypes.c_int
+    lib.fs_attention_forward.argtypes = [fmtp, i32, i32, i64, i64, ctypes.c_float, mp, mp, mp, biasp, dropp, mp, vp, vp, sz, vp]
+    lib.fs_attention_backward_workspace_bytes.restype = ctypes.c_int
+    lib.fs_attention_backward_workspace_bytes.argtypes = [fmtp, fmtp, i32, i32, i64, i64, i32, szp]
+    lib.fs_attention_backward.restype = ctypes.c_int
+    lib.fs_attention_backward.argtypes = [fmtp, fmtp, i32, i32, i64, i64, ctypes.c_float, mp, mp, mp, biasp, dropp, mp, vp, mp, mp, mp, mp,
+                                          vp, vp, sz, vp]
     lib.fs_blk_to_csr.restype = ctypes.c_int
     lib.fs_blk_to_csr.argtypes = [fmtp, vp, vp, vp]
     lib.fs_csr_to_blk.restype = ctypes.c_int
@@ -534,6 +565,204 @@ def _attention_like(name, fmt, X, Y, H, scale, out, work, stream):
     if rc:
         raise FsError(rc, name)
     return out
+
+
+class FsBucketBias:
+    """A learned bias of the scores by relative position, column - row - ``shift``.
+
+    ``table``: (heads, buckets) in the element type, or (buckets,) for a single head; ``buckets``: uint8, the bucket of the relative
+    positions -reach .. reach (2 * reach + 1 values, longer distances count as reach).  ``fs_relative_buckets`` makes one."""
+
+    def __init__(self, table, buckets, shift: int = 0):
+        assert table.is_cuda and table.dim() in (1, 2) and table.stride(-1) == 1 and table.element_size() == 2
+        assert buckets.is_cuda and buckets.dtype == torch.uint8 and buckets.dim() == 1 and buckets.is_contiguous() and buckets.numel() % 2 == 1
+        self.table, self.buckets, self.shift = table, buckets, int(shift)
+
+    def _struct(self, fmt, heads):
+        t = self.table
+        assert t.dtype == fmt.torch_dtype and (t.shape[0] if t.dim() == 2 else 1) == heads and t.stride(-1) == 1
+        return _FsBucketBiasStruct(t.data_ptr(), t.stride(0) if t.dim() == 2 and heads > 1 else t.shape[-1], self.buckets.data_ptr(), t.shape[-1],
+                                   self.buckets.numel() // 2, self.shift)
+
+
+class FsDropout:
+    """Dropout with probability ``p``; ``state``: int64 on the GPU, {seed, step}, read when the kernels run.  The mask of an entry
+    follows from seed, step, head, row and column, so a backward call with the same state draws that of the forward call; a
+    program adds one to ``state[1]`` after both (in a captured graph too)."""
+
+    def __init__(self, p: float, state):
+        assert state.is_cuda and state.dtype == torch.int64 and state.numel() == 2 and state.is_contiguous()
+        self.p, self.state = float(p), state
+
+    def _struct(self):
+        return _FsDropoutStruct(self.p, self.state.data_ptr())
+
+
+def fs_relative_buckets(buckets: int, max_distance: int, bidirectional: bool = True, device="cuda"):
+    """The usual table of buckets for relative positions -max_distance .. max_distance: distances below half of the buckets of a
+    direction have one each, longer ones share logarithmically wide ones, from ``max_distance`` on the last.  ``bidirectional``:
+    half of the buckets are for columns behind the row; else all are for columns up to the row, and those behind it count as
+    distance zero.  The borders are exact (integer comparisons, no logarithms)."""
+    n = buckets // 2 if bidirectional else buckets
+    near = n // 2
+    if not (near >= 1 and near < max_distance <= 1024 and buckets <= 128 and (not bidirectional or buckets % 2 == 0)):
+        raise ValueError("no such buckets")
+    of = list(range(near))  # by distance
+    for dist in range(near, max_distance + 1):  # largest k with (dist / near)^(n - near) >= (max_distance / near)^k
+        k = of[-1] - near if dist > near else 0
+        while k < n - near - 1 and dist ** (n - near) * near ** (k + 1) >= max_distance ** (k + 1) * near ** (n - near):
+            k += 1
+        of.append(near + k)
+    behind = [n + b for b in of[1:]] if bidirectional else [0] * max_distance
+    return torch.tensor(of[:0:-1] + [0] + behind, dtype=torch.uint8, device=device)
+
+
+def _value_heads(fmt, vals):
+    """Number of value arrays in (V*nvec,) or (heads, V*nvec)."""
+    assert vals.is_cuda and vals.dtype == fmt.torch_dtype and vals.is_contiguous() and vals.dim() in (1, 2)
+    assert vals.shape[-1] == fmt.c.V * fmt.c.nvec
+    return vals.shape[0] if vals.dim() == 2 else 1
+
+
+def fs_edge_bias(fmt: FsFormat, vals, bias: FsBucketBias, scale: float = 1.0, out=None, stream=None):
+    """scale * value + the bias of the entry, on vals_blk-layout arrays, one or (heads, V*nvec) (out may be vals)."""
+    heads = _value_heads(fmt, vals)
+    if out is None:
+        out = torch.empty_like(vals)
+    assert out.shape == vals.shape and out.dtype == vals.dtype and out.is_contiguous()
+    rc = load_library().fs_edge_bias(ctypes.byref(fmt.c), heads, vals.data_ptr(), float(scale), ctypes.byref(bias._struct(fmt, heads)), out.data_ptr(),
+                                     _stream_ptr(stream))
+    if rc:
+        raise FsError(rc, "fs_edge_bias")
+    return out
+
+
+def fs_edge_bias_backward_workspace_bytes(fmt: FsFormat, heads: int, n_buckets: int) -> int:
+    n = ctypes.c_size_t(0)
+    rc = load_library().fs_edge_bias_backward_workspace_bytes(ctypes.byref(fmt.c), heads, n_buckets, ctypes.byref(n))
+    if rc:
+        raise FsError(rc, "fs_edge_bias_backward_workspace_bytes")
+    return int(n.value)
+
+
+def fs_edge_bias_backward(fmt: FsFormat, grad, bias: FsBucketBias, out=None, work=None, stream=None):
+    """Gradient of the bias table from the gradient of fs_edge_bias's result (the gradient of its values is scale * grad):
+    (heads, buckets), or (buckets,) for a single array."""
+    heads = _value_heads(fmt, grad)
+    n_buckets = bias.table.shape[-1]
+    if out is None:
+        out = grad.new_empty((heads, n_buckets) if grad.dim() == 2 else (n_buckets,))
+    assert out.numel() == heads * n_buckets and out.dtype == grad.dtype and out.is_contiguous() and out.is_cuda
+    if work is None:
+        work = _temporary(max(fs_edge_bias_backward_workspace_bytes(fmt, heads, n_buckets), 16), grad, stream)
+    rc = load_library().fs_edge_bias_backward(ctypes.byref(fmt.c), heads, grad.data_ptr(), ctypes.byref(bias._struct(fmt, heads)), out.data_ptr(),
+                                              work.data_ptr(), work.numel() * work.element_size(), _stream_ptr(stream))
+    if rc:
+        raise FsError(rc, "fs_edge_bias_backward")
+    return out
+
+
+def fs_edge_dropout(fmt: FsFormat, vals, dropout: FsDropout, out=None, stream=None):
+    """Dropout on vals_blk-layout arrays, one or (heads, V*nvec): the probabilities in the forward pass, their gradient in the
+    backward pass (out may be vals)."""
+    heads = _value_heads(fmt, vals)
+    if out is None:
+        out = torch.empty_like(vals)
+    assert out.shape == vals.shape and out.dtype == vals.dtype and out.is_contiguous()
+    rc = load_library().fs_edge_dropout(ctypes.byref(fmt.c), heads, vals.data_ptr(), ctypes.byref(dropout._struct()), out.data_ptr(), _stream_ptr(stream))
+    if rc:
+        raise FsError(rc, "fs_edge_dropout")
+    return out
+
+
+def _head_matrix(t, fmt, rows):
+    """(rows, columns) or (rows, heads, columns) -> (struct, heads, columns)."""
+    assert t.is_cuda and t.dtype == fmt.torch_dtype and t.dim() in (2, 3) and t.shape[0] == rows and t.stride(-1) == 1
+    heads, columns = (t.shape[1], t.shape[2]) if t.dim() == 3 else (1, t.shape[1])
+    return (_FsHeadMatrix(t.data_ptr(), t.stride(0) if rows > 1 else max(t.stride(0), columns), t.stride(1) if heads > 1 else 0 if t.dim() == 2 else columns),
+            heads, columns)
+
+
+def fs_attention_forward_workspace_bytes(fmt: FsFormat, heads: int, N: int) -> int:
+    n = ctypes.c_size_t(0)
+    rc = load_library().fs_attention_forward_workspace_bytes(ctypes.byref(fmt.c), heads, N, ctypes.byref(n))
+    if rc:
+        raise FsError(rc, "fs_attention_forward_workspace_bytes")
+    return int(n.value)
+
+
+def _attention_operands(fmt, X, Y, H, bias, dropout):
+    x, heads, d = _head_matrix(X, fmt, fmt.c.M)
+    y, kv_heads, dy = _head_matrix(Y, fmt, fmt.c.K)
+    h, hv, N = _head_matrix(H, fmt, fmt.c.K)
+    assert dy == d and hv == kv_heads and X.dim() == Y.dim() == H.dim()
+    return (heads, kv_heads, d, N, x, y, h, None if bias is None else ctypes.byref(bias._struct(fmt, heads)),
+            None if dropout is None else ctypes.byref(dropout._struct()))
+
+
+def fs_attention_forward(fmt: FsFormat, X, Y, H, scale: float = 1.0, bias: Optional[FsBucketBias] = None, dropout: Optional[FsDropout] = None, out=None,
+                         lse=None, work=None, stream=None):
+    """dropout(softmax_rows(scale * (X @ Y.T) + bias at A's stored positions)) @ H for every head, and the log-sum-exp of the rows.
+
+    X: (M, d) or (M, heads, d); Y: (K, d) or (K, kv_heads, d), H the same with N columns; a query head h reads
+    keys and values h // (heads // kv_heads).  Returns (out, lse): like X with N columns, and float32 (M,) or (heads, M)."""
+    heads, kv_heads, d, N, x, y, h, b, dr = _attention_operands(fmt, X, Y, H, bias, dropout)
+    M = fmt.c.M
+    if out is None:
+        out = X.new_empty((M, N) if X.dim() == 2 else (M, heads, N))
+    assert out.dim() == X.dim()
+    o, oh, oN = _head_matrix(out, fmt, M)
+    assert oh == heads and oN == N
+    if lse is None:
+        lse = torch.empty((M,) if X.dim() == 2 else (heads, M), dtype=torch.float32, device=X.device)
+    assert lse.is_cuda and lse.dtype == torch.float32 and lse.numel() == heads * M and lse.is_contiguous()
+    work, work_ptr, work_bytes = _workspace(fmt, work, X, stream, fs_attention_forward_workspace_bytes, heads, N)
+    rc = load_library().fs_attention_forward(ctypes.byref(fmt.c), heads, kv_heads, d, N, float(scale), ctypes.byref(x), ctypes.byref(y), ctypes.byref(h), b, dr,
+                                             ctypes.byref(o), lse.data_ptr(), work_ptr, work_bytes, _stream_ptr(stream))
+    if rc:
+        raise FsError(rc, "fs_attention_forward")
+    return out, lse
+
+
+def fs_attention_backward_workspace_bytes(fmt: FsFormat, fmt_t: FsFormat, heads: int, kv_heads: int, d: int, N: int, n_buckets: int = 0) -> int:
+    n = ctypes.c_size_t(0)
+    rc = load_library().fs_attention_backward_workspace_bytes(ctypes.byref(fmt.c), ctypes.byref(fmt_t.c), heads, kv_heads, d, N, n_buckets, ctypes.byref(n))
+    if rc:
+        raise FsError(rc, "fs_attention_backward_workspace_bytes")
+    return int(n.value)
+
+
+def fs_attention_backward(fmt: FsFormat, fmt_t: FsFormat, X, Y, H, out, lse, grad, scale: float = 1.0, bias: Optional[FsBucketBias] = None,
+                          dropout: Optional[FsDropout] = None, dX=None, dY=None, dH=None, dTable=None, work=None, stream=None):
+    """The gradients of fs_attention_forward, whose ``out`` and ``lse`` these are, from the gradient ``grad`` of out: (dX, dY, dH,
+    dTable), the last None without a bias.  ``fmt_t`` is the format of A^T (fs_csr_transpose, fs_convert)."""
+    heads, kv_heads, d, N, x, y, h, b, dr = _attention_operands(fmt, X, Y, H, bias, dropout)
+    M = fmt.c.M
+    assert out.dim() == grad.dim() == X.dim()
+    o, oh, oN = _head_matrix(out, fmt, M)
+    g, gh, gN = _head_matrix(grad, fmt, M)
+    assert oh == gh == heads and oN == gN == N
+    assert lse.is_cuda and lse.dtype == torch.float32 and lse.numel() == heads * M and lse.is_contiguous()
+    dX = X.new_empty(X.shape) if dX is None else dX
+    dY = Y.new_empty(Y.shape) if dY is None else dY
+    dH = H.new_empty(H.shape) if dH is None else dH
+    assert dX.shape == X.shape and dY.shape == Y.shape and dH.shape == H.shape
+    n_buckets = 0
+    if bias is not None:
+        n_buckets = bias.table.shape[-1]
+        dTable = bias.table.new_empty(bias.table.shape) if dTable is None else dTable
+        assert dTable.shape == bias.table.shape and dTable.dtype == bias.table.dtype and dTable.is_contiguous() and dTable.is_cuda
+    else:
+        assert dTable is None
+    if work is None:
+        work = _temporary(max(fs_attention_backward_workspace_bytes(fmt, fmt_t, heads, kv_heads, d, N, n_buckets), 16), X, stream)
+    rc = load_library().fs_attention_backward(
+        ctypes.byref(fmt.c), ctypes.byref(fmt_t.c), heads, kv_heads, d, N, float(scale), ctypes.byref(x), ctypes.byref(y), ctypes.byref(h), b, dr,
+        ctypes.byref(o), lse.data_ptr(), ctypes.byref(g), *(ctypes.byref(_head_matrix(t, fmt, r)[0]) for t, r in ((dX, M), (dY, fmt.c.K), (dH, fmt.c.K))),
+        None if dTable is None else dTable.data_ptr(), work.data_ptr(), work.numel() * work.element_size(), _stream_ptr(stream))
+    if rc:
+        raise FsError(rc, "fs_attention_backward")
+    return dX, dY, dH, dTable
 
 
 def fs_blk_to_csr(fmt: FsFormat, blk, out=None, stream=None):

@@ -7,7 +7,7 @@ from concurrent.futures import ThreadPoolExecutor
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(_HERE)
-SOURCES = ["fs_convert.hip", "fs_spmm.hip", "fs_sddmm.hip", "fs_softmax.hip", "fs_attention.hip", "fs_transpose.hip", "fs_api.hip"]
+SOURCES = ["fs_convert.hip", "fs_spmm.hip", "fs_sddmm.hip", "fs_softmax.hip", "fs_attention.hip", "fs_edges.hip", "fs_heads.hip", "fs_heads_backward.hip", "fs_transpose.hip", "fs_api.hip"]
 LIB = os.path.join(_HERE, "libflashsparse_hip.so")
 CALLS_SRC = os.path.join(_HERE, "csrc", "fs_torch.cpp")
 CALLS_LIB = os.path.join(_HERE, "_fs_torch.so")

@@ -1,5 +1,5 @@
 // Argument checking for the compute entry points of the C ABI; the kernels live in
-// fs_spmm.hip / fs_sddmm.hip / fs_softmax.hip / fs_attention.hip, conversion and utilities in fs_convert.hip.
+// fs_spmm.hip / fs_sddmm.hip / fs_softmax.hip / fs_attention.hip / fs_edges.hip / fs_heads.hip / fs_heads_backward.hip, conversion and utilities in fs_convert.hip.
 #include <algorithm>
 #include <mutex>
 
@@ -326,6 +326,170 @@ extern "C" fs_status fs_sddmm_spmm(const fs_format *fmt, const void *d_X, int64_
                                    int64_t ldo, void *d_work, size_t work_bytes, void *stream)
 {
     return attention_call(fmt, d_X, ldx, d_Y, ldy, d, scale, d_H, N, ldh, d_out, ldo, d_work, work_bytes, stream, false);
+}
+
+// ------------------------------------------------------------------- several heads, a bucket bias, dropout and the gradients
+namespace {
+
+constexpr int kMostHeads = 65535;   // the second dimension of a grid
+constexpr int kMostShared = 64;     // query heads for one of keys and values
+
+fs_status bias_arguments(const fs_bucket_bias *b, bool reads_table)
+{
+    if (!b) return FS_OK;
+    if (b->n_buckets < 1 || b->reach < 0 || !b->d_bucket || !aligned(b->d_bucket, 4)) return FS_ERR_INVALID_ARG;
+    if (reads_table && (!b->d_table || !aligned(b->d_table, 2) || (b->ld != 0 && b->ld < b->n_buckets))) return FS_ERR_INVALID_ARG;
+    if (b->shift <= -((int64_t)1 << 31) || b->shift >= ((int64_t)1 << 31)) return FS_ERR_INVALID_ARG;
+    return b->n_buckets <= 128 && b->reach <= 1024 ? FS_OK : FS_ERR_UNSUPPORTED;
+}
+
+fs_status drop_arguments(const fs_dropout *d)
+{
+    if (!d) return FS_OK;
+    if (!(d->p >= 0.0 && d->p < 1.0)) return FS_ERR_INVALID_ARG;  // (nor a NaN)
+    return d->p == 0.0 || (d->d_state && aligned(d->d_state, 8)) ? FS_OK : FS_ERR_INVALID_ARG;
+}
+
+// A matrix per head of rows x columns.  The kernels address its rows with 32-bit byte offsets formed by a 24-bit multiply.
+fs_status matrix_arguments(const fs_head_matrix *m, int64_t rows, int64_t columns, int heads, bool written)
+{
+    if (!m || m->ld < columns || m->head < 0 || m->ld % 8 || m->head % 8) return FS_ERR_INVALID_ARG;
+    if (written && heads > 1 && m->head < columns) return FS_ERR_INVALID_ARG;
+    if (rows > 0 && (!m->d || !aligned(m->d, 16))) return FS_ERR_INVALID_ARG;
+    const int64_t lim24 = (int64_t)1 << 24, lim32 = (int64_t)1 << 32;
+    return m->ld * 2 < lim24 && rows * m->ld * 2 < lim32 && m->head < ((int64_t)1 << 46) ? FS_OK : FS_ERR_UNSUPPORTED;
+}
+
+// What the two attention calls have in common.
+fs_status heads_arguments(const fs_format *f, int32_t heads, int32_t kv_heads, int64_t d, int64_t N, float scale, const fs_head_matrix *X,
+                          const fs_head_matrix *Y, const fs_head_matrix *H, const fs_head_matrix *out, bool out_written, const fs_bucket_bias *bias,
+                          const fs_dropout *drop)
+{
+    if (!format_ok(f) || heads < 1 || kv_heads < 1 || heads % kv_heads || d < 8 || N < 8 || d % 8 || N % 8) return FS_ERR_INVALID_ARG;
+    if (!(scale == scale) || scale - scale != 0.f) return FS_ERR_INVALID_ARG;  // NaN, infinity
+    if (!kernels_support(f) || d > 128 || N > 128 || heads > kMostHeads || heads / kv_heads > kMostShared) return FS_ERR_UNSUPPORTED;
+    if (f->M >= ((int64_t)1 << 24) || f->K >= ((int64_t)1 << 24)) return FS_ERR_UNSUPPORTED;
+    if (f->n_items > 0 && !f->blk_row_bits) return FS_ERR_INVALID_ARG;
+    fs_status s = bias_arguments(bias, true);
+    if (s == FS_OK) s = drop_arguments(drop);
+    if (s == FS_OK) s = matrix_arguments(X, f->M, d, heads, false);
+    if (s == FS_OK) s = matrix_arguments(Y, f->K, d, kv_heads, false);
+    if (s == FS_OK) s = matrix_arguments(H, f->K, N, kv_heads, false);
+    if (s == FS_OK) s = matrix_arguments(out, f->M, N, heads, out_written);
+    return s;
+}
+
+fs_status workspace_arguments(const void *d_work, size_t work_bytes, size_t need)
+{
+    if (need > 0 && (!d_work || !aligned(d_work, 16))) return FS_ERR_INVALID_ARG;
+    return work_bytes < need ? FS_ERR_BUFFER_TOO_SMALL : FS_OK;
+}
+
+fs_status edge_arguments(const fs_format *f, int32_t heads, const void *d_in, const void *d_out, bool out_needed)
+{
+    if (!format_ok(f) || heads < 0) return FS_ERR_INVALID_ARG;
+    if (!kernels_support(f) || heads > kMostHeads) return FS_ERR_UNSUPPORTED;
+    if (heads == 0 || f->nvec == 0) return FS_OK;
+    if (!f->blk_row_bits || !d_in || !aligned(d_in, 2) || (out_needed && (!d_out || !aligned(d_out, 2)))) return FS_ERR_INVALID_ARG;
+    return FS_OK;
+}
+
+}  // namespace
+
+extern "C" fs_status fs_edge_bias(const fs_format *fmt, int32_t heads, const void *d_in_blk, float scale, const fs_bucket_bias *bias,
+                                  void *d_out_blk, void *stream)
+{
+    if (!bias || !(scale == scale) || scale - scale != 0.f) return FS_ERR_INVALID_ARG;
+    fs_status s = edge_arguments(fmt, heads, d_in_blk, d_out_blk, true);
+    if (s == FS_OK) s = bias_arguments(bias, true);
+    if (s != FS_OK || heads == 0 || fmt->nvec == 0) return s;
+    return fs_edge_bias_launch(fmt, heads, d_in_blk, scale, bias, d_out_blk, (hipStream_t)stream);
+}
+
+extern "C" fs_status fs_edge_bias_backward_workspace_bytes(const fs_format *fmt, int32_t heads, int32_t n_buckets, size_t *work_bytes)
+{
+    if (!format_ok(fmt) || !work_bytes || heads < 0 || n_buckets < 0) return FS_ERR_INVALID_ARG;
+    if (!kernels_support(fmt) || heads > kMostHeads || n_buckets > 128) return FS_ERR_UNSUPPORTED;
+    *work_bytes = fmt->nvec > 0 ? fs_edge_bias_backward_floats(fmt, heads, n_buckets) * sizeof(float) : 0;
+    return FS_OK;
+}
+
+extern "C" fs_status fs_edge_bias_backward(const fs_format *fmt, int32_t heads, const void *d_g_blk, const fs_bucket_bias *bias,
+                                           void *d_table_grad, void *d_work, size_t work_bytes, void *stream)
+{
+    if (!bias) return FS_ERR_INVALID_ARG;
+    fs_status s = edge_arguments(fmt, heads, d_g_blk, nullptr, false);
+    if (s == FS_OK) s = bias_arguments(bias, false);
+    if (s != FS_OK || heads == 0) return s;
+    if (!d_table_grad || !aligned(d_table_grad, 2)) return FS_ERR_INVALID_ARG;
+    size_t need = 0;
+    fs_edge_bias_backward_workspace_bytes(fmt, heads, bias->n_buckets, &need);
+    s = workspace_arguments(d_work, work_bytes, need);
+    return s != FS_OK ? s : fs_edge_bias_backward_launch(fmt, heads, d_g_blk, bias, d_table_grad, d_work, (hipStream_t)stream);
+}
+
+extern "C" fs_status fs_edge_dropout(const fs_format *fmt, int32_t heads, const void *d_in_blk, const fs_dropout *drop, void *d_out_blk, void *stream)
+{
+    if (!drop) return FS_ERR_INVALID_ARG;
+    fs_status s = edge_arguments(fmt, heads, d_in_blk, d_out_blk, true);
+    if (s == FS_OK) s = drop_arguments(drop);
+    if (s != FS_OK || heads == 0 || fmt->nvec == 0) return s;
+    return fs_edge_dropout_launch(fmt, heads, d_in_blk, drop, d_out_blk, (hipStream_t)stream);
+}
+
+extern "C" fs_status fs_attention_forward_workspace_bytes(const fs_format *fmt, int32_t heads, int64_t N, size_t *work_bytes)
+{
+    if (!format_ok(fmt) || !work_bytes || heads < 1 || N < 0) return FS_ERR_INVALID_ARG;
+    *work_bytes = fs_attention_forward_floats(fmt, heads, N) * sizeof(float);
+    return FS_OK;
+}
+
+extern "C" fs_status fs_attention_forward(const fs_format *fmt, int32_t heads, int32_t kv_heads, int64_t d, int64_t N, float scale,
+                                          const fs_head_matrix *X, const fs_head_matrix *Y, const fs_head_matrix *H, const fs_bucket_bias *bias,
+                                          const fs_dropout *drop, const fs_head_matrix *out, float *d_lse, void *d_work, size_t work_bytes, void *stream)
+{
+    fs_status s = heads_arguments(fmt, heads, kv_heads, d, N, scale, X, Y, H, out, true, bias, drop);
+    if (s != FS_OK || fmt->M == 0) return s;
+    if (!aligned(d_lse, 4)) return FS_ERR_INVALID_ARG;
+    s = workspace_arguments(d_work, work_bytes, fs_attention_forward_floats(fmt, heads, N) * sizeof(float));
+    if (s != FS_OK) return s;
+    return fs_attention_forward_launch(fmt, heads, kv_heads, (int)d, (int)N, scale, X, Y, H, bias, drop, out, d_lse, d_work, (hipStream_t)stream);
+}
+
+static bool transposed_format(const fs_format *f, const fs_format *t)
+{
+    return format_ok(t) && t->M == f->K && t->K == f->M && t->nnz == f->nnz && t->dtype == f->dtype && (t->n_items == 0 || t->blk_row_bits);
+}
+
+extern "C" fs_status fs_attention_backward_workspace_bytes(const fs_format *fmt, const fs_format *fmt_t, int32_t heads, int32_t kv_heads, int64_t d,
+                                                           int64_t N, int32_t n_buckets, size_t *work_bytes)
+{
+    if (!format_ok(fmt) || !format_ok(fmt_t) || !work_bytes || heads < 1 || kv_heads < 1 || d < 0 || N < 0 || n_buckets < 0) return FS_ERR_INVALID_ARG;
+    *work_bytes = fs_attention_backward_floats(fmt, fmt_t, heads, kv_heads, d, N, n_buckets) * sizeof(float);
+    return FS_OK;
+}
+
+extern "C" fs_status fs_attention_backward(const fs_format *fmt, const fs_format *fmt_t, int32_t heads, int32_t kv_heads, int64_t d, int64_t N, float scale,
+                                           const fs_head_matrix *X, const fs_head_matrix *Y, const fs_head_matrix *H, const fs_bucket_bias *bias,
+                                           const fs_dropout *drop, const fs_head_matrix *out, const float *d_lse, const fs_head_matrix *G,
+                                           const fs_head_matrix *dX, const fs_head_matrix *dY, const fs_head_matrix *dH, void *d_table_grad,
+                                           void *d_work, size_t work_bytes, void *stream)
+{
+    fs_status s = heads_arguments(fmt, heads, kv_heads, d, N, scale, X, Y, H, out, false, bias, drop);
+    if (s != FS_OK) return s;
+    if (!transposed_format(fmt, fmt_t)) return FS_ERR_INVALID_ARG;
+    if (!kernels_support(fmt_t)) return FS_ERR_UNSUPPORTED;
+    s = matrix_arguments(G, fmt->M, N, heads, false);
+    if (s == FS_OK) s = matrix_arguments(dX, fmt->M, d, heads, true);
+    if (s == FS_OK) s = matrix_arguments(dY, fmt->K, d, kv_heads, true);
+    if (s == FS_OK) s = matrix_arguments(dH, fmt->K, N, kv_heads, true);
+    if (s != FS_OK) return s;
+    if ((fmt->M > 0 && !d_lse) || !aligned(d_lse, 4) || (d_table_grad && !bias) || !aligned(d_table_grad, 2)) return FS_ERR_INVALID_ARG;
+    const size_t need = fs_attention_backward_floats(fmt, fmt_t, heads, kv_heads, d, N, d_table_grad ? bias->n_buckets : 0) * sizeof(float);
+    s = workspace_arguments(d_work, work_bytes, need);
+    if (s != FS_OK) return s;
+    return fs_attention_backward_launch(fmt, fmt_t, heads, kv_heads, (int)d, (int)N, scale, X, Y, H, bias, drop, out, d_lse, G, dX, dY, dH, d_table_grad, d_work,
+                                        (hipStream_t)stream);
 }
 
 extern "C" fs_status fs_read_bytes(const void *d_src, size_t bytes, int32_t repeats, void *d_sink, size_t sink_bytes, void *stream)

@@ -119,3 +119,20 @@ fs_status fs_edge_softmax_launch(const fs_format *fmt, const void *d_in_blk, voi
                                  void *d_work, hipStream_t stream);
 fs_status fs_edge_softmax_backward_launch(const fs_format *fmt, const void *d_p_blk, const void *d_g_blk, void *d_out_blk,
                                           float scale, void *d_work, hipStream_t st);
+fs_status fs_edge_bias_launch(const fs_format *fmt, int heads, const void *d_in, float scale, const fs_bucket_bias *bias, void *d_out, hipStream_t st);
+fs_status fs_edge_bias_backward_launch(const fs_format *fmt, int heads, const void *d_g, const fs_bucket_bias *bias, void *d_grad, void *d_work,
+                                       hipStream_t st);
+size_t fs_edge_bias_backward_floats(const fs_format *fmt, int heads, int n_buckets);
+fs_status fs_edge_dropout_launch(const fs_format *fmt, int heads, const void *d_in, const fs_dropout *drop, void *d_out, hipStream_t st);
+size_t fs_attention_forward_floats(const fs_format *fmt, int64_t heads, int64_t N);
+fs_status fs_attention_forward_launch(const fs_format *fmt, int heads, int kv_heads, int d, int N, float scale, const fs_head_matrix *X,
+                                      const fs_head_matrix *Y, const fs_head_matrix *H, const fs_bucket_bias *bias, const fs_dropout *drop,
+                                      const fs_head_matrix *out, float *d_lse, void *d_work, hipStream_t st);
+size_t fs_attention_backward_floats(const fs_format *fmt, const fs_format *fmt_t, int64_t heads, int64_t kv_heads, int64_t d, int64_t N, int64_t n_buckets);
+fs_status fs_attention_backward_launch(const fs_format *fmt, const fs_format *fmt_t, int heads, int kv_heads, int d, int N, float scale,
+                                       const fs_head_matrix *X, const fs_head_matrix *Y, const fs_head_matrix *H, const fs_bucket_bias *bias,
+                                       const fs_dropout *drop, const fs_head_matrix *out, const float *d_lse, const fs_head_matrix *G,
+                                       const fs_head_matrix *dX, const fs_head_matrix *dY, const fs_head_matrix *dH, void *d_table_grad, void *d_work,
+                                       hipStream_t st);
+// rows x columns zeros for every head (columns % 8 == 0), and minus infinity in rows x heads floats (null: none)
+fs_status fs_zero_heads_launch(const fs_head_matrix *m, int64_t rows, int64_t columns, int heads, float *d_lse, hipStream_t st);

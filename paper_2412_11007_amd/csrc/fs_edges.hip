@@ -1,0 +1,226 @@
+// A bucket bias and dropout on value arrays in the vals_blk layout, and the gradient of the bias table.
+//
+// bias      out = scale * in + table[bucket(column - row - shift)]
+// dropout   out = in * factor where the entry is kept, else zero (and the same on a gradient)
+// gradient  dtable[k] = sum of g over the entries of bucket k
+//
+// A block is V x kb consecutive elements, row by row.  A lane takes eight of them, sixteen bytes, so that a wave-wide load or store
+// moves 1 KB of consecutive blocks (16 / V of them at full width) whatever their width; the row and the place of an element
+// follow from its number and kb.  Which elements A stores is read from blk_row_bits, the columns of the block's vectors from
+// vec_col; both pass through LDS.
+//
+// The gradient adds into a table in LDS of n_buckets x 64 fp32 sums, one column a lane: no two lanes share an address, the sums
+// of a lane are added in the order in which its wavefront walks the blocks, and at the end the columns of a bucket are added in a
+// fixed order.  The wavefronts' tables are added by a second launch, so the result does not depend on timing.
+#include <algorithm>
+
+#include "fs_common.h"
+#include "fs_heads.h"
+#include "fs_tile.h"
+
+namespace {
+
+enum { OP_BIAS = 0, OP_DROPOUT = 1, OP_GRADIENT = 2 };
+
+constexpr int kWaves = 4;  // of a workgroup; OP_GRADIENT: one
+
+template <int DT, int V, int OP>
+__global__ void __launch_bounds__(OP == OP_GRADIENT ? 64 : 64 * kWaves)
+k_edges(const int4 *__restrict__ blk_desc, int n_blocks, const uint32_t *__restrict__ row_bits, const int32_t *__restrict__ vec_col, int nvec,
+        const uint16_t *in, uint16_t *out, int64_t n_el, float scale, fs_bias_args bias, fs_drop_args drop, float *__restrict__ sums)
+{
+    constexpr int WAVES = OP == OP_GRADIENT ? 1 : kWaves;
+    constexpr int PER = 16 / V;    // blocks of a round
+    constexpr int LANES = 4 * V;   // lanes of a block
+    __shared__ __attribute__((aligned(16))) int cols_all[WAVES][PER][32];
+    __shared__ uint32_t bits_all[WAVES][16];
+    extern __shared__ __attribute__((aligned(16))) unsigned char dyn[];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, head = blockIdx.y;
+    float *table = reinterpret_cast<float *>(dyn);                   // OP_BIAS: of the head
+    uint8_t *lut = dyn + (OP == OP_BIAS ? bias.n_buckets * 4 : 0);
+    float *mine = reinterpret_cast<float *>(dyn + (2 * bias.reach + 1 + 15) / 16 * 16) + lane;  // OP_GRADIENT: + 64 * bucket
+    fs_key key = fs_key{0u, 0u};
+    if constexpr (OP == OP_DROPOUT) {
+        key = fs_drop_key(drop, head);
+    } else {
+        fs_load_buckets(bias, lut, threadIdx.x, WAVES * 64);
+        if constexpr (OP == OP_BIAS) {
+            for (int i = threadIdx.x; i < bias.n_buckets; i += WAVES * 64) table[i] = fs_widen<DT>(bias.table[head * bias.ld + i]);
+        } else {
+            for (int i = 0; i < bias.n_buckets; i++) mine[64 * i] = 0.f;
+        }
+        __syncthreads();
+    }
+    in += head * n_el;
+    if constexpr (OP != OP_GRADIENT) out += head * n_el;
+    int *cols = cols_all[wave][lane / LANES];
+    uint32_t *bits = bits_all[wave] + (lane / LANES) * V;
+    const int e0 = 8 * (lane % LANES);  // of the block
+
+    const int step = gridDim.x * WAVES * PER;
+    for (int x0 = (blockIdx.x * WAVES + wave) * PER; x0 < n_blocks; x0 += step) {
+        const int x = x0 + lane / LANES;
+        const int4 desc = blk_desc[min(x, n_blocks - 1)];
+        const int kb = x < n_blocks ? desc.y & 255 : 0;
+        const int64_t first = (int64_t)V * desc.x;
+        const int own = min(8, V * kb - e0);  // elements of the lane: eight, four (V = 4, odd width) or none
+        fs_frag v;
+        v.u = fs_u4{0u, 0u, 0u, 0u};
+        if (own == 8) v.u = *reinterpret_cast<const fs_u4_unaligned *>(in + first + e0);
+        else if (own == 4) v.s[0] = __builtin_bit_cast(fs_s4, *reinterpret_cast<const fs_u2_unaligned *>(in + first + e0));
+        // the block's columns, and its rows' occupancy
+        for (int c = lane % LANES; c < 32; c += LANES) cols[c] = vec_col[max(min(desc.x + min(c, kb - 1), nvec - 1), 0)];
+        if (lane % LANES < V) bits[lane % LANES] = row_bits[(int64_t)min(x, n_blocks - 1) * V + lane % LANES];
+        FS_WAVE_SYNC();
+        const uint32_t inv = kb == 32 ? 2048u : (uint32_t)(65536.f * __builtin_amdgcn_rcpf((float)max(kb, 1))) + 1u;  // e / kb = e * inv >> 16 for e < 512
+        auto row_of = [&](int k) -> int { return min((int)((uint32_t)(e0 + k) * inv >> 16), V - 1); };
+        uint32_t m8 = 0;
+        if (kb == 32) {
+            m8 = bits[e0 >> 5] >> (e0 & 31) & 255u;
+        } else if (own > 0) {
+#pragma unroll
+            for (int k = 0; k < 8; k++) {
+                const int r = row_of(k);
+                if (k < own) m8 |= (bits[r] >> (e0 + k - r * kb) & 1u) << k;
+            }
+        }
+        const int row0 = desc.z * V;
+        if constexpr (OP == OP_DROPOUT) {
+            const uint32_t kept = fs_kept(m8, key, drop.below, [&](int k) -> int2 {
+                const int r = row_of(k);
+                return make_int2(row0 + r, cols[e0 + k - r * kb]);
+            });
+            float y[8];
+#pragma unroll
+            for (int k = 0; k < 8; k++) y[k] = kept >> k & 1u ? fs_widen<DT>(v.e[k]) * drop.factor : 0.f;
+            v.u = fs_u4{fs_pack2<DT>(y[0], y[1]), fs_pack2<DT>(y[2], y[3]), fs_pack2<DT>(y[4], y[5]), fs_pack2<DT>(y[6], y[7])};
+        } else {
+            float y[8];
+#pragma unroll
+            for (int k = 0; k < 8; k++) {
+                y[k] = 0.f;
+                if (m8 >> k & 1u) {
+                    const int r = row_of(k);
+                    const int b = fs_bucket_of(lut, bias.reach, bias.shift, row0 + r, cols[e0 + k - r * kb]);
+                    if constexpr (OP == OP_BIAS) y[k] = fmaf(scale, fs_widen<DT>(v.e[k]), table[b]);
+                    else fs_lds_add(mine + 64 * b, fs_widen<DT>(v.e[k]));
+                }
+            }
+            if constexpr (OP == OP_BIAS) v.u = fs_u4{fs_pack2<DT>(y[0], y[1]), fs_pack2<DT>(y[2], y[3]), fs_pack2<DT>(y[4], y[5]), fs_pack2<DT>(y[6], y[7])};
+        }
+        if constexpr (OP != OP_GRADIENT) {
+            if (own == 8) *reinterpret_cast<fs_u4_unaligned *>(out + first + e0) = v.u;
+            else if (own == 4) *reinterpret_cast<fs_u2_unaligned *>(out + first + e0) = __builtin_bit_cast(fs_u2, v.s[0]);
+        }
+        FS_WAVE_SYNC();
+    }
+    if constexpr (OP == OP_GRADIENT) {
+        float *to = sums + ((int64_t)head * gridDim.x + blockIdx.x) * bias.n_buckets;
+        FS_WAVE_SYNC();
+        fs_store_bucket_sums<64>(mine - lane, bias.n_buckets, lane, to);
+    }
+}
+
+// Adds n tables of n_buckets sums, a contiguous share of them per workgroup: thread (r, b) those r, r + R, ... of its share, R = 256
+// over the buckets' power of two; then the R sums of a bucket in order.  DT < 0: to fp32 tables, one a workgroup.
+template <int DT>
+__global__ void __launch_bounds__(256) k_bucket_sums(const float *__restrict__ sums, int n, int n_buckets, int log2_buckets, void *__restrict__ to)
+{
+    __shared__ float part[256];
+    const int b = threadIdx.x & ((1 << log2_buckets) - 1), r = threadIdx.x >> log2_buckets, R = 256 >> log2_buckets;
+    const int head = blockIdx.y, share = (n + gridDim.x - 1) / gridDim.x, i0 = blockIdx.x * share, i1 = min(n, i0 + share);
+    const float *from = sums + (int64_t)head * n * n_buckets + min(b, n_buckets - 1);
+    float t = 0.f;
+    for (int i = i0 + r; i < i1; i += 8 * R) {
+        float v[8];
+#pragma unroll
+        for (int k = 0; k < 8; k++) v[k] = from[(int64_t)min(i + k * R, i1 - 1) * n_buckets];
+#pragma unroll
+        for (int k = 0; k < 8; k++) t += i + k * R < i1 ? v[k] : 0.f;
+    }
+    part[threadIdx.x] = t;
+    __syncthreads();
+    if (r > 0 || b >= n_buckets) return;
+    for (int k = 1; k < R; k++) t += part[(k << log2_buckets) + b];
+    const int64_t at = ((int64_t)head * gridDim.x + blockIdx.x) * n_buckets + b;
+    if constexpr (DT < 0) ((float *)to)[at] = t;
+    else ((uint16_t *)to)[at] = fs_round_bits<DT>(t);
+}
+
+template <int DT, int V, int OP>
+fs_status launch(const fs_format *f, int heads, const uint16_t *in, uint16_t *out, float scale, const fs_bias_args &bias,
+                 const fs_drop_args &drop, float *work, hipStream_t st)
+{
+    const int64_t rounds = f->nvec > 0 ? (f->n_blocks + 16 / V - 1) / (16 / V) : 0;
+    const int lut = (2 * bias.reach + 1 + 15) / 16 * 16;
+    if constexpr (OP == OP_GRADIENT) {
+        const unsigned waves = (unsigned)std::min<int64_t>(rounds, fs_edge_gradient_waves(heads));
+        if (waves > 0)
+            k_edges<DT, V, OP><<<dim3(waves, heads), 64, lut + 256 * bias.n_buckets, st>>>((const int4 *)f->blk_desc, (int)f->n_blocks, f->blk_row_bits, f->vec_col, (int)f->nvec,
+                                                                                        in, nullptr, (int64_t)V * f->nvec, scale, bias, drop, work);
+        FS_LAUNCH_CHECK();
+        return fs_bucket_sums_launch(f->dtype, heads, (int)waves, bias.n_buckets, work, out, st);
+    }
+    if (rounds == 0) return FS_OK;
+    const unsigned groups = (unsigned)std::min<int64_t>((rounds + kWaves - 1) / kWaves, 256 * 8);
+    k_edges<DT, V, OP><<<dim3(groups, heads), 64 * kWaves, OP == OP_BIAS ? lut + 4 * bias.n_buckets : 0, st>>>(
+        (const int4 *)f->blk_desc, (int)f->n_blocks, f->blk_row_bits, f->vec_col, (int)f->nvec, in, out, (int64_t)V * f->nvec, scale, bias, drop, nullptr);
+    FS_LAUNCH_CHECK();
+    return FS_OK;
+}
+
+template <int OP>
+fs_status launch_any(const fs_format *f, int heads, const void *in, void *out, float scale, const fs_bias_args &bias, const fs_drop_args &drop,
+                     void *work, hipStream_t st)
+{
+#define FS_EDGES(DT, ROWS) \
+    if (f->dtype == DT && f->V == ROWS) return launch<DT, ROWS, OP>(f, heads, (const uint16_t *)in, (uint16_t *)out, scale, bias, drop, (float *)work, st)
+    FS_EDGES(FS_F16, 4);
+    FS_EDGES(FS_F16, 8);
+    FS_EDGES(FS_F16, 16);
+    FS_EDGES(FS_BF16, 4);
+    FS_EDGES(FS_BF16, 8);
+    FS_EDGES(FS_BF16, 16);
+#undef FS_EDGES
+    return FS_ERR_UNSUPPORTED;
+}
+
+}  // namespace
+
+fs_status fs_bucket_sums_launch(int dtype, int heads, int n, int n_buckets, float *sums, void *grad, hipStream_t st)
+{
+    int log2_buckets = 0;
+    while (1 << log2_buckets < n_buckets) log2_buckets++;
+    if (n > 4 * kBucketSumGroups) {
+        float *part = sums + (size_t)heads * n * n_buckets;
+        k_bucket_sums<-1><<<dim3(kBucketSumGroups, heads), 256, 0, st>>>(sums, n, n_buckets, log2_buckets, part);
+        FS_LAUNCH_CHECK();
+        sums = part;
+        n = kBucketSumGroups;
+    }
+    if (dtype == FS_BF16) k_bucket_sums<FS_BF16><<<dim3(1, heads), 256, 0, st>>>(sums, n, n_buckets, log2_buckets, grad);
+    else k_bucket_sums<FS_F16><<<dim3(1, heads), 256, 0, st>>>(sums, n, n_buckets, log2_buckets, grad);
+    FS_LAUNCH_CHECK();
+    return FS_OK;
+}
+
+fs_status fs_edge_bias_launch(const fs_format *f, int heads, const void *in, float scale, const fs_bucket_bias *b, void *out, hipStream_t st)
+{
+    return launch_any<OP_BIAS>(f, heads, in, out, scale, fs_bias_of(b), fs_drop_of(nullptr), nullptr, st);
+}
+
+fs_status fs_edge_dropout_launch(const fs_format *f, int heads, const void *in, const fs_dropout *d, void *out, hipStream_t st)
+{
+    return launch_any<OP_DROPOUT>(f, heads, in, out, 1.f, fs_bias_of(nullptr), fs_drop_of(d), nullptr, st);
+}
+
+size_t fs_edge_bias_backward_floats(const fs_format *f, int heads, int n_buckets)
+{
+    const int64_t rounds = (f->n_blocks + 16 / f->V - 1) / (16 / f->V);
+    return fs_bucket_sums_floats(heads, std::min<int64_t>(rounds, fs_edge_gradient_waves(heads)), n_buckets);
+}
+
+fs_status fs_edge_bias_backward_launch(const fs_format *f, int heads, const void *g, const fs_bucket_bias *b, void *grad, void *work, hipStream_t st)
+{
+    return launch_any<OP_GRADIENT>(f, heads, g, grad, 1.f, fs_bias_of(b), fs_drop_of(nullptr), work, st);
+}

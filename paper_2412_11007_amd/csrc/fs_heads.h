@@ -1,0 +1,389 @@
+// Device pieces shared by the kernels of attention with several heads, a bucket bias and dropout (fs_heads.hip,
+// fs_heads_backward.hip) and by the same steps on value arrays (fs_edges.hip).
+//
+// Bias.  The bias of an entry is that of the bucket of its clamped relative position column - row - shift.  The buckets of
+// all 2 * reach + 1 positions are a table of bytes that the caller made (any rule, exact at its borders); it and the head's
+// biases, widened to fp32, are copied to LDS when a workgroup starts, so that an entry costs two LDS reads.
+//
+// Dropout.  An entry is dropped where a word drawn for (head, row, column) is below p * 2^32.  The generator is Threefry-2x32
+// (Salmon, Moraes, Dror, Shaw, "Parallel random numbers: as easy as 1, 2, 3", 2011): additions, rotations and exclusive ors,
+// all of them full-rate instructions here (a Philox of the same paper takes 20 quarter-rate multiplications a call), with the 13
+// rounds that the paper reports to pass its batteries for entries and the default 20 for keys.  The counter is (row, column): no
+// mask is stored, and the kernels that walk A by rows, those that walk A^T and the ones on value arrays draw the same one.
+#pragma once
+
+#include <algorithm>
+
+#include "fs_common.h"
+#include "fs_tile.h"
+
+namespace {
+
+template <int DT>
+__device__ __forceinline__ float fs_widen(uint16_t bits)
+{
+    if (DT == FS_F16) return (float)__builtin_bit_cast(_Float16, bits);
+    return __uint_as_float((uint32_t)bits << 16);
+}
+
+struct fs_key {
+    uint32_t k0, k1;
+};
+
+// Threefry-2x32: both words of the counter (c0, c1) under a key.
+template <int ROUNDS>
+__host__ __device__ __forceinline__ fs_key fs_threefry(fs_key key, uint32_t c0, uint32_t c1)
+{
+    constexpr int turn[8] = {13, 15, 26, 6, 17, 29, 16, 24};
+    const uint32_t ks[3] = {key.k0, key.k1, key.k0 ^ key.k1 ^ 0x1BD11BDAu};
+    uint32_t a = c0 + key.k0, b = c1 + key.k1;
+#pragma unroll
+    for (int i = 0; i < ROUNDS; i++) {
+        a += b;
+        b = (b << turn[i % 8] | b >> (32 - turn[i % 8])) ^ a;
+        if (i % 4 == 3) {
+            a += ks[(i / 4 + 1) % 3];
+            b += ks[(i / 4 + 2) % 3] + (uint32_t)(i / 4 + 1);
+        }
+    }
+    return fs_key{a, b};
+}
+
+// What the kernels are given of a bias and of a dropout (n_buckets = 0, state null: none).
+struct fs_bias_args {
+    const uint16_t *table;
+    const uint8_t *bucket;
+    int64_t ld;
+    int n_buckets, reach, shift;
+};
+struct fs_drop_args {
+    const int64_t *state;  // seed and step
+    uint32_t below;        // an entry whose word is below is dropped
+    float factor;          // 1 / (1 - p)
+};
+
+__device__ __forceinline__ fs_key fs_drop_key(const fs_drop_args &d, int head)
+{
+    fs_key k = fs_key{0u, 0u};
+    if (d.state) {
+        const uint64_t seed = (uint64_t)d.state[0], step = (uint64_t)d.state[1];
+        k = fs_threefry<20>(fs_key{(uint32_t)seed, (uint32_t)(seed >> 32)}, (uint32_t)step, (uint32_t)(step >> 32));
+        k = fs_threefry<20>(k, (uint32_t)head, 0u);
+    }
+    return fs_key{(uint32_t)__builtin_amdgcn_readfirstlane((int)k.k0), (uint32_t)__builtin_amdgcn_readfirstlane((int)k.k1)};
+}
+
+// Bytes of LDS for a head's biases and the buckets of the positions.
+__host__ __device__ __forceinline__ int fs_bias_lds_bytes(int n_buckets, int reach)
+{
+    return n_buckets > 0 ? n_buckets * 4 + (2 * reach + 1 + 3) / 4 * 4 : 0;
+}
+
+// The buckets of the positions as bytes, four at a time (`bucket` is 4-byte aligned), no index past the table's end.
+__device__ __forceinline__ void fs_load_buckets(const fs_bias_args &b, uint8_t *lut, int thread, int threads)
+{
+    const int n = 2 * b.reach + 1;
+    const uint32_t most = (uint32_t)b.n_buckets - 1;
+    for (int i = thread; i < (n + 3) / 4; i += threads) {
+        uint32_t v = 0;
+        if (4 * i + 4 <= n) v = reinterpret_cast<const uint32_t *>(b.bucket)[i];
+        else
+            for (int k = 0; 4 * i + k < n; k++) v |= (uint32_t)b.bucket[4 * i + k] << (8 * k);
+        uint32_t o = 0;
+#pragma unroll
+        for (int k = 0; k < 4; k++) o |= min(v >> (8 * k) & 255u, most) << (8 * k);
+        reinterpret_cast<uint32_t *>(lut)[i] = o;
+    }
+}
+
+// Bucket of the entry (row, col).  Rows and columns are below 2^31; the subtraction of the shift saturates.
+__device__ __forceinline__ int fs_bucket_of(const uint8_t *lut, int reach, int shift, int row, int col)
+{
+    const int r = __builtin_elementwise_sub_sat(col - row, shift);
+    return lut[min(max(r, -reach), reach) + reach];
+}
+
+// Which of a lane's eight positions (m8: those that are stored) are kept.  at(x): the counter of position x.
+template <typename Counter>
+__device__ __forceinline__ uint32_t fs_kept(uint32_t m8, fs_key key, uint32_t below, Counter at)
+{
+    uint32_t kept = 0;
+    for (uint32_t m = m8; m; m &= m - 1) {
+        const int x = __builtin_ctz(m);
+        const int2 c = at(x);  // row, column of A
+        if (fs_threefry<13>(key, (uint32_t)c.x, (uint32_t)c.y).k0 >= below) kept |= 1u << x;
+    }
+    return kept;
+}
+
+// Adds to a lane's own cell of a table in LDS (one instruction, nothing to wait for).
+__device__ __forceinline__ void fs_lds_add(float *cell, float v) { unsafeAtomicAdd(cell, v); }
+
+// A wavefront's table of COLS sums per bucket (a power of two) -> one sum per bucket.  The order of the columns differs from
+// bucket to bucket, so that the lanes read different banks, and is always the same.
+template <int COLS>
+__device__ __forceinline__ void fs_store_bucket_sums(const float *table, int n_buckets, int lane, float *__restrict__ to)
+{
+    for (int b = lane; b < n_buckets; b += 64) {
+        float t = 0.f;
+#pragma unroll 8
+        for (int c = 0; c < COLS; c++) t += table[COLS * b + ((c + b) & (COLS - 1))];
+        to[b] = t;
+    }
+}
+
+// ln 2 * (m + log2 l): the log-sum-exp of a row whose scores, in units of log2, have the maximum m and the sum l of 2^(. - m).
+// A row without entries, or with nothing but minus infinities, has minus infinity.
+__device__ __forceinline__ float fs_log_sum(float m, float l)
+{
+    return l == 0.f ? -INFINITY : 0.693147180559945309f * (m + __builtin_amdgcn_logf(l));
+}
+
+// Host side: the checked arguments as the kernels take them.
+inline fs_bias_args fs_bias_of(const fs_bucket_bias *b)
+{
+    if (!b) return fs_bias_args{nullptr, nullptr, 0, 0, 0, 0};
+    return fs_bias_args{(const uint16_t *)b->d_table, b->d_bucket, b->ld, b->n_buckets, b->reach, (int)b->shift};
+}
+inline fs_drop_args fs_drop_of(const fs_dropout *d)
+{
+    if (!d || d->p == 0.0) return fs_drop_args{nullptr, 0u, 1.f};
+    return fs_drop_args{d->d_state, (uint32_t)(d->p * 4294967296.0), (float)(1.0 / (1.0 - d->p))};
+}
+
+// Wavefronts for one head's gradient of a bias table on a value array: enough to fill the chip (a table of 32 buckets takes
+// 8 KB of LDS, twenty of them a CU), few enough that their tables are soon added.
+inline int fs_edge_gradient_waves(int heads) { return std::max(256, 4096 / std::max(heads, 1)); }
+
+// Sums over `n` tables go through this many partial ones (0: straight).
+constexpr int kBucketSumGroups = 64;
+inline size_t fs_bucket_sums_floats(int64_t heads, int64_t n, int64_t n_buckets) { return (size_t)heads * (size_t)(n + kBucketSumGroups) * (size_t)n_buckets; }
+
+}  // namespace
+
+// grad[h][b] = sum over i < n of sums[h][i][b], rounded to the element type; `sums` is followed by room for the partial ones
+// (fs_bucket_sums_floats in all).  In fs_edges.hip.
+fs_status fs_bucket_sums_launch(int dtype, int heads, int n, int n_buckets, float *sums, void *grad, hipStream_t st);
+
+// ---------------------------------------------------------------------------------------------------------------------------
+// The block walk of the attention kernels
+
+namespace {
+
+// The work list and the pattern, as the kernels take them.
+struct fs_walk {
+    const int4 *items;
+    const int4 *blk_desc;
+    const int32_t *vec_col;
+    const uint32_t *row_bits;
+    int64_t M;
+    int n_items, nvec, n_slots, slice, n_swz;
+};
+inline fs_walk fs_walk_of(const fs_format *f, const fs_launch_geometry &geo)
+{
+    return fs_walk{(const int4 *)f->items_by_cost, (const int4 *)f->blk_desc, f->vec_col, f->blk_row_bits, f->M,
+                   (int)f->n_items, (int)f->nvec, (int)f->n_split_items, geo.slice, geo.n_swz};
+}
+
+// A matrix per head whose rows are gathered or held: byte strides.
+struct fs_operand {
+    unsigned char *p;
+    int64_t head;
+    uint32_t pitch;
+};
+inline fs_operand fs_operand_of(const fs_head_matrix *m) { return fs_operand{(unsigned char *)m->d, 2 * m->head, (uint32_t)(2 * m->ld)}; }
+
+// 32 gathered rows of up to NC columns on their way to LDS: 16 bytes a lane, neighbouring lanes on one row; in LDS the layout of the
+// staged tile (lds_row), where they are read as they are (contraction over the columns) and transposed (over the rows).
+// Columns from `width` on are zeros.
+template <int NC>
+struct fs_gathered {
+    static constexpr int LPR = NC / 8, RPI = 64 / LPR, NLD = 32 / RPI, RS = NC * 2;
+    static constexpr int kBytes = (lds_row<RS>(31) + RS + 15) / 16 * 16;
+    fs_u4 r[NLD];
+
+    // cols: lane l holds the row number of vector l (mod 32); colb: the lane's column_bytes()
+    __device__ __forceinline__ void load(const unsigned char *base, uint32_t pitch, uint32_t colb, int cols, int lane)
+    {
+#pragma unroll
+        for (int l = 0; l < NLD; l++) {
+            const int row = __shfl(cols, l * RPI + lane / LPR, 64);
+            r[l] = *reinterpret_cast<const fs_u4 *>(base + (fs_mul24((uint32_t)row, pitch) + colb));
+        }
+    }
+    static __device__ __forceinline__ uint32_t column_bytes(int lane, int width) { return 2 * (uint32_t)min((lane % LPR) * 8, width - 8); }
+    __device__ __forceinline__ void put(unsigned char *lds, int lane, int width) const
+    {
+        const bool in = (lane % LPR) * 8 < width;
+        unsigned char *to = lds + lds_row<RS>(lane / LPR) + (lane % LPR) * 16;
+#pragma unroll
+        for (int l = 0; l < NLD; l++) *reinterpret_cast<fs_u4 *>(to + lds_row<RS>(l * RPI)) = in ? r[l] : fs_u4{0u, 0u, 0u, 0u};
+    }
+    // tile t of the products with an operand held in registers: lane (j, g) gets vectors 8g + 4t .. +3 of window row j
+    template <int DT, int STEPS>
+    static __device__ __forceinline__ fs_f4 contract(const unsigned char *lds, int t, int lane, const fs_frag (&held)[STEPS])
+    {
+        const int j = lane & 15, g = lane >> 4;
+        const unsigned char *rd = lds + lds_row<RS>(8 * (j >> 2) + (j & 3)) + 4 * t * (RS + 32) + 16 * g;
+        fs_f4 acc = fs_f4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int ks = 0; ks < STEPS; ks++) {
+            fs_frag a;
+            a.u = *reinterpret_cast<const fs_u4 *>(rd + 64 * ks);
+            acc = fs_mfma_16x16x32<DT>(a, held[ks], acc);
+        }
+        return acc;
+    }
+    // 16-column tile t, transposed: the operand that is multiplied with a weight per (vector, window row)
+    static __device__ __forceinline__ fs_frag transposed(const unsigned char *lds, int t, int lane)
+    {
+        const int g = lane >> 4;
+        const unsigned char *rd = lds + lds_row<RS>(8 * g + ((lane & 15) >> 2)) + 8 * (lane & 3);
+        fs_frag a;
+#pragma unroll
+        for (int h = 0; h < 2; h++)
+            a.s[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((fs_s4 __attribute__((address_space(3))) *)(rd + lds_row<RS>(4 * h) + 32 * t));
+        return a;
+    }
+};
+
+// A window's rows in operand layout: lane (j, g) holds columns 32ks + 8g .. +7 of row w * V + j; rows past V or the last, and columns
+// past `width`, are zeros.
+template <int V, int STEPS>
+__device__ __forceinline__ void fs_load_window(fs_frag (&held)[STEPS], const unsigned char *base, uint32_t pitch, int width, int w, int64_t rows, int lane)
+{
+    const int j = lane & 15, g = lane >> 4;
+    const int64_t row = (int64_t)w * V + j;
+    const bool ok = j < V && row < rows;
+    const unsigned char *at = base + fs_mul24((uint32_t)(ok ? row : 0), pitch);
+#pragma unroll
+    for (int ks = 0; ks < STEPS; ks++) {
+        const bool in = 32 * ks + 8 * g < width;
+        held[ks].u = *reinterpret_cast<const fs_u4 *>(at + (in ? 2 * (32 * ks + 8 * g) : 0));
+        if (!ok || !in) held[ks].u = fs_u4{0u, 0u, 0u, 0u};
+    }
+}
+
+// The columns of a block's vectors, lane l that of vector l mod 32; vectors past the block's width repeat its last one.
+__device__ __forceinline__ int fs_block_cols(const fs_walk &a, const BlockDesc &b, int lane)
+{
+    return a.vec_col[max(min(b.s + min(lane & 31, b.kb - 1), a.nvec - 1), 0)];
+}
+
+// Occupancy of window row j in block i of an item: the eight vectors 8g .. 8g+7 of the lane (none for lanes past V).
+template <int V>
+__device__ __forceinline__ uint32_t fs_lane_bits(const fs_walk &a, int first_slot, int i, int nblk, int lane)
+{
+    const int j = lane & 15, g = lane >> 4;
+    const uint32_t m = a.row_bits[(int64_t)(first_slot + min(i, nblk - 1)) * V + (j & (V - 1))];
+    return i < nblk && j < V ? m >> (8 * g) & 255u : 0u;
+}
+
+template <int NT>
+__device__ __forceinline__ void fs_clear(fs_f4 (&acc)[NT])
+{
+#pragma unroll
+    for (int t = 0; t < NT; t++) acc[t] = fs_f4{0.f, 0.f, 0.f, 0.f};
+}
+
+template <int DT>
+__device__ __forceinline__ fs_frag fs_round8(const float (&p)[8])
+{
+    fs_frag o;
+    o.u = fs_u4{fs_pack2<DT>(p[0], p[1]), fs_pack2<DT>(p[2], p[3]), fs_pack2<DT>(p[4], p[5]), fs_pack2<DT>(p[6], p[7])};
+    return o;
+}
+
+// Accumulators -> rounded rows of an output of up to NC columns, by way of the tile's LDS.
+template <int DT, int V, int NC>
+__device__ __forceinline__ void fs_store_window(unsigned char *lds, const fs_f4 (&acc)[NC / 16], float factor, unsigned char *base, uint32_t pitch,
+                                                int width, int w, int64_t rows, int lane)
+{
+    using tile = fs_gathered<NC>;
+    FS_WAVE_SYNC();
+    fs_round_tile_to_lds<DT, V, NC / 16, tile::RS>(lds, acc, lane & 15, lane >> 4, factor);
+    FS_WAVE_SYNC();
+    fs_store_tile_rows<V, tile::RPI, tile::RS>(lds + lds_row<tile::RS>(lane / tile::LPR) + (lane % tile::LPR) * 16, (uint16_t *)base, pitch / 2, w, rows,
+                                               width, lane / tile::LPR, (lane % tile::LPR) * 8);
+    FS_WAVE_SYNC();
+}
+
+// Accumulators -> partial tile `slot` of a head's tiles of `width` columns.
+template <int V, int NT>
+__device__ __forceinline__ void fs_store_part(float *tiles, int slot, int width, const fs_f4 (&acc)[NT], int lane)
+{
+    const int j = lane & 15, g = lane >> 4;
+    fs_store_partial_tile<V, NT>(tiles, slot, width, (uint32_t)((g * V + j) * 16), acc, j < V, NT * 16 <= width, 0, g);
+}
+
+// Adds the partial tiles of one cut window and 32 columns, in slot order, one wavefront each, for every head.  SM: the parts carry
+// (maximum m, sum l) per row of a softmax in units of log2, and with m* the largest m of a row
+//   out = factor * sum_k 2^(m_k - m*) tile_k / sum_k 2^(m_k - m*) l_k,   lse = ln 2 * (m* + log2 of that sum).
+// Lane (row r = lane % V, q = lane / V) first walks the parts q, q + 64/V, ...; tiles are read in their storage order, sixteen loads in
+// flight, and the rounded rows leave through LDS.
+template <int DT, int V, bool SM>
+__global__ void __launch_bounds__(64)
+k_add_parts(const int4 *__restrict__ split_windows, const float *__restrict__ part, const float *__restrict__ stats, int n_slots, int N,
+            fs_operand out, float factor, int64_t M, float *__restrict__ lse)
+{
+    constexpr int CH = 32, KQ = 64 / V;
+    __shared__ __attribute__((aligned(16))) uint16_t out_t[V][CH + 8];
+    const int n_chunks = (N + CH - 1) / CH, head = blockIdx.y;
+    const int4 sw = split_windows[blockIdx.x / n_chunks];
+    const int w = sw.x, p0 = sw.y, cnt = sw.z;
+    const int lane = threadIdx.x, r = lane % V, q = lane / V;
+    const int c0 = (blockIdx.x % n_chunks) * CH, nc = min(CH, N - c0);
+    const float *st = SM ? stats + ((int64_t)head * n_slots + p0) * 2 * V : nullptr;
+    float use = 0.f, inv = factor;
+    if constexpr (SM) {
+        float top = -INFINITY;
+        for (int k = q; k < cnt; k += KQ) top = fmaxf(top, st[(int64_t)k * 2 * V + r]);
+#pragma unroll
+        for (int o = V; o < 64; o <<= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
+        use = top == -INFINITY ? 0.f : top;
+        float total = 0.f;
+        for (int k = q; k < cnt; k += KQ) total += st[(int64_t)k * 2 * V + V + r] * __builtin_amdgcn_exp2f(st[(int64_t)k * 2 * V + r] - use);
+#pragma unroll
+        for (int o = V; o < 64; o <<= 1) total += __shfl_xor(total, o, 64);
+        inv = total == 0.f ? 0.f : factor / total;
+        if (lse && c0 == 0 && q == 0 && (int64_t)w * V + r < M) lse[(int64_t)head * M + (int64_t)w * V + r] = fs_log_sum(use, total);
+    }
+    const int64_t tile4 = (int64_t)V * N / 4;
+    const fs_f4 *src0 = reinterpret_cast<const fs_f4 *>(part) + ((int64_t)head * n_slots + p0) * tile4 + (c0 / 4) * V;
+    for (int idx = lane; idx < (nc / 4) * V; idx += 64) {  // idx % V == r
+        const int ct = idx / (4 * V), rem = idx - ct * 4 * V, g = rem / V, j = rem - g * V;
+        const fs_f4 *src = src0 + idx;
+        fs_f4 sum = fs_f4{0.f, 0.f, 0.f, 0.f};
+        for (int k = 0; k < cnt; k += 16) {
+            fs_f4 v[16];
+            float wk[16];
+#pragma unroll
+            for (int u = 0; u < 16; u++) {
+                const int kk = min(k + u, cnt - 1);
+                v[u] = src[(int64_t)kk * tile4];
+                wk[u] = SM ? st[(int64_t)kk * 2 * V + j] : 0.f;
+            }
+#pragma unroll
+            for (int u = 0; u < 16; u++)
+                if (k + u < cnt) sum += SM ? v[u] * __builtin_amdgcn_exp2f(wk[u] - use) : v[u];
+        }
+        uint2 o;
+        o.x = fs_pack2<DT>(sum[0] * inv, sum[1] * inv);
+        o.y = fs_pack2<DT>(sum[2] * inv, sum[3] * inv);
+        *reinterpret_cast<uint2 *>(&out_t[j][16 * ct + 4 * g]) = o;
+    }
+    __syncthreads();
+    const int c8n = nc / 8;
+    for (int t = lane; t < V * c8n; t += 64) {
+        const int j = t / c8n, c8 = t - j * c8n;
+        const int64_t row = (int64_t)w * V + j;
+        if (row < M)
+            __builtin_nontemporal_store(*reinterpret_cast<const fs_u4 *>(&out_t[j][8 * c8]),
+                                        reinterpret_cast<fs_u4 *>(out.p + head * out.head + row * out.pitch + 2 * (c0 + 8 * c8)));
+    }
+}
+
+// Floats of the partial tiles of one kernel.
+inline size_t fs_part_floats(const fs_format *f, int64_t heads, int64_t columns) { return (size_t)heads * (size_t)f->n_split_items * (size_t)f->V * (size_t)columns; }
+
+}  // namespace

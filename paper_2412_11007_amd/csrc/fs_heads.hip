@@ -1,0 +1,230 @@
+// Attention with several heads, a bucket bias and dropout, and the rows' log-sum-exp: the forward pass of training, and (without
+// dropout) that of serving.
+//
+//   s = scale * x_i . y_j + bias(j - i),  out_i = sum over the stored j of dropout(softmax(s)) h_j,  lse_i = log sum exp(s)
+//
+// A wavefront walks one item of the work list for one head, block by block (32 vectors of a window of V rows):
+//   * the 32 rows of Y and of H are gathered row by row and put to LDS while the ones before are computed with;
+//   * the scores of the V x 32 block come from the matrix cores, Y's rows as the left operand and the window's rows of X, held in
+//     registers, as the right one: lane (j, g) gets the scores of window row j and vectors 8g .. 8g+7;
+//   * bias and pattern are applied in fp32 in units of log2, the running maximum m and sum l of the row are updated, the
+//     probabilities that dropout keeps are rounded to the element type relative to m;
+//   * they meet H's rows, read transposed from LDS, on the matrix cores; the accumulators are scaled by 2^(m_old - m_new).
+// At a window's end the tile is divided by l (1 / (1 - p) goes in with it) and stored; parts of a cut window leave fp32 tiles and
+// (m, l), which k_add_parts merges in slot order.  l counts what dropout takes out as well: the mask applies after the softmax.
+// Heads are the slower grid dimension, so that one head's rows of Y and H share the L2s; query heads with the same keys are neighbours.
+#include <type_traits>
+
+#include "fs_common.h"
+#include "fs_heads.h"
+
+namespace {
+
+template <int DT, int V, int KS, int NT>
+__global__ void __launch_bounds__(64)
+k_heads_forward(fs_walk a, fs_operand X, fs_operand Y, fs_operand H, int share, int d, int N, float sl2, fs_bias_args bias, fs_drop_args drop,
+                fs_operand out, float *__restrict__ lse, float *__restrict__ part, float *__restrict__ stats)
+{
+    using tile_y = fs_gathered<32 * KS>;
+    using tile_h = fs_gathered<16 * NT>;
+    __shared__ __attribute__((aligned(16))) unsigned char lds_y[tile_y::kBytes];
+    __shared__ __attribute__((aligned(16))) unsigned char lds_h[tile_h::kBytes];
+    __shared__ __attribute__((aligned(16))) int lds_cols[32];
+    extern __shared__ __attribute__((aligned(16))) unsigned char dyn[];
+    float *table = reinterpret_cast<float *>(dyn);
+    uint8_t *lut = dyn + 4 * bias.n_buckets;
+
+    const int lane = threadIdx.x, head = blockIdx.y;
+    const int turn = __builtin_amdgcn_readfirstlane(fs_launch_turn<1>(blockIdx.x, a.slice, a.n_swz));
+    if (turn >= a.n_items) return;
+    const int4 it = a.items[turn];
+    const int nblk = it.y;
+    if (nblk == 0) return;
+    int slot = it.z;
+    const int j = lane & 15, g = lane >> 4;
+    const int4 my_desc = a.blk_desc[it.x + min(lane, nblk - 1)];
+    auto block = [&](int i) -> BlockDesc { return fs_item_block(my_desc, i, nblk); };
+    const unsigned char *Xb = X.p + head * X.head, *Yb = Y.p + head / share * Y.head, *Hb = H.p + head / share * H.head;
+    const uint32_t y_colb = tile_y::column_bytes(lane, d), h_colb = tile_h::column_bytes(lane, N);
+
+    BlockDesc d0 = block(0), d1 = block(1);
+    int cols0 = fs_block_cols(a, d0, lane), cols1 = fs_block_cols(a, d1, lane);
+    uint32_t bits0 = fs_lane_bits<V>(a, it.x, 0, nblk, lane);
+    fs_frag xf[KS];
+    fs_load_window<V>(xf, Xb, X.pitch, d, d0.w, a.M, lane);
+    tile_y y;
+    tile_h h;
+    y.load(Yb, Y.pitch, y_colb, cols0, lane);
+    h.load(Hb, H.pitch, h_colb, cols0, lane);
+    if (bias.n_buckets > 0) {
+        fs_load_buckets(bias, lut, lane, 64);
+        for (int i = lane; i < bias.n_buckets; i += 64) table[i] = fs_widen<DT>(bias.table[head * bias.ld + i]) * 1.44269504088896340736f;
+    }
+    const fs_key key = fs_drop_key(drop, head);
+
+    fs_f4 acc[NT];
+    fs_clear(acc);
+    float m_run = -INFINITY, l_run = 0.f;  // l_run: this lane's share
+    bool from_first = d0.first;
+    int step = 0;
+    auto block_step = [&](auto more_) {
+        constexpr bool MORE = decltype(more_)::value;
+        y.put(lds_y, lane, d);
+        h.put(lds_h, lane, N);
+        if (lane < 32) lds_cols[lane] = cols0;
+        const BlockDesc d2 = block(step + 2);
+        int cols2 = 0;
+        uint32_t bits1 = 0;
+        if constexpr (MORE) {
+            y.load(Yb, Y.pitch, y_colb, cols1, lane);
+            h.load(Hb, H.pitch, h_colb, cols1, lane);
+            cols2 = fs_block_cols(a, d2, lane);
+            bits1 = fs_lane_bits<V>(a, it.x, step + 1, nblk, lane);
+        }
+        FS_WAVE_SYNC();
+        fs_f4 sc[2];
+#pragma unroll
+        for (int t = 0; t < 2; t++) sc[t] = tile_y::template contract<DT>(lds_y, t, lane, xf);
+        const int row = d0.w * V + j;
+        float p[8], mx = -INFINITY;
+#pragma unroll
+        for (int x = 0; x < 8; x++) {
+            float t = sc[x >> 2][x & 3] * sl2;
+            if (bias.n_buckets > 0) t += table[fs_bucket_of(lut, bias.reach, bias.shift, row, lds_cols[8 * g + x])];
+            p[x] = bits0 >> x & 1u ? t : -INFINITY;
+            mx = fmaxf(mx, p[x]);
+        }
+        mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+        mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+        const float m_new = fmaxf(m_run, mx);
+        const float m_use = m_new == -INFINITY ? 0.f : m_new;  // nothing seen so far
+        const float corr = __builtin_amdgcn_exp2f(m_run - m_use);
+        float ps = 0.f;
+#pragma unroll
+        for (int x = 0; x < 8; x++) {
+            p[x] = __builtin_amdgcn_exp2f(p[x] - m_use);
+            ps += p[x];
+        }
+        l_run = l_run * corr + ps;
+        m_run = m_new;
+        if (drop.state) {
+            const uint32_t kept = fs_kept(bits0, key, drop.below, [&](int x) -> int2 { return make_int2(row, lds_cols[8 * g + x]); });
+#pragma unroll
+            for (int x = 0; x < 8; x++) p[x] = kept >> x & 1u ? p[x] : 0.f;
+        }
+        const fs_frag sp = fs_round8<DT>(p);
+        if (d0.kb > 0) {
+#pragma unroll
+            for (int t = 0; t < NT; t++) acc[t] = fs_mfma_16x16x32<DT>(tile_h::transposed(lds_h, t, lane), sp, acc[t] * corr);
+        }
+        FS_WAVE_SYNC();
+        if (MORE && d1.w != d0.w) fs_load_window<V>(xf, Xb, X.pitch, d, d1.w, a.M, lane);
+        if (d0.last || !MORE) {
+            float l_tot = l_run + __shfl_xor(l_run, 16, 64);
+            l_tot += __shfl_xor(l_tot, 32, 64);
+            if (d0.last && from_first) {
+                fs_store_window<DT, V, 16 * NT>(lds_h, acc, l_tot == 0.f ? 0.f : drop.factor / l_tot, out.p + head * out.head, out.pitch, N, d0.w, a.M, lane);
+                if (lse && g == 0 && j < V && row < a.M) lse[(int64_t)head * a.M + row] = fs_log_sum(m_run, l_tot);
+            } else {
+                fs_store_part<V>(part + (int64_t)head * a.n_slots * V * N, slot, N, acc, lane);
+                if (g == 0 && j < V) {
+                    float *st = stats + ((int64_t)head * a.n_slots + slot) * 2 * V;
+                    st[j] = m_run;
+                    st[V + j] = l_tot;
+                }
+                slot++;
+            }
+            fs_clear(acc);
+            m_run = -INFINITY;
+            l_run = 0.f;
+        }
+        if (d0.last) from_first = true;
+        d0 = d1;
+        d1 = d2;
+        cols0 = cols1;
+        cols1 = cols2;
+        bits0 = bits1;
+    };
+    for (; step + 1 < nblk; step++) block_step(std::true_type{});
+    block_step(std::false_type{});
+}
+
+__global__ void __launch_bounds__(256) k_zero_heads(fs_operand m, int64_t rows, int pieces, float *__restrict__ lse)
+{
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, row = i / pieces;
+    if (row >= rows) return;
+    const int c = (int)(i - row * pieces);
+    *reinterpret_cast<fs_u4 *>(m.p + blockIdx.y * m.head + row * m.pitch + 16 * c) = fs_u4{0u, 0u, 0u, 0u};
+    if (lse && c == 0) lse[blockIdx.y * rows + row] = -INFINITY;
+}
+
+struct call {
+    int heads, share, d, N;
+    float sl2;
+    fs_operand X, Y, H, out;
+    fs_bias_args bias;
+    fs_drop_args drop;
+    float *lse, *work;
+    hipStream_t st;
+};
+
+template <int DT, int V, int KS, int NT>
+fs_status launch(const fs_format *f, const call &c)
+{
+    const fs_launch_geometry geo = fs_launch_geometry_for(f, 1);
+    const fs_walk a = fs_walk_of(f, geo);
+    float *stats = c.work + fs_part_floats(f, c.heads, c.N);
+    k_heads_forward<DT, V, KS, NT><<<dim3(geo.nbx, c.heads), 64, fs_bias_lds_bytes(c.bias.n_buckets, c.bias.reach), c.st>>>(
+        a, c.X, c.Y, c.H, c.share, c.d, c.N, c.sl2, c.bias, c.drop, c.out, c.lse, c.work, stats);
+    FS_LAUNCH_CHECK();
+    if (f->n_split_windows > 0) {
+        const int64_t blocks = f->n_split_windows * ((c.N + 31) / 32);
+        if (blocks >= ((int64_t)1 << 31)) return FS_ERR_TOO_LARGE;
+        k_add_parts<DT, V, true><<<dim3((unsigned)blocks, c.heads), 64, 0, c.st>>>((const int4 *)f->split_windows, c.work, stats, (int)f->n_split_items, c.N,
+                                                                                  c.out, c.drop.factor, f->M, c.lse);
+        FS_LAUNCH_CHECK();
+    }
+    return FS_OK;
+}
+
+template <int DT, int V, int KS>
+fs_status launch_n(const fs_format *f, const call &c)
+{
+    return c.N <= 32 ? launch<DT, V, KS, 2>(f, c) : c.N <= 64 ? launch<DT, V, KS, 4>(f, c) : launch<DT, V, KS, 8>(f, c);
+}
+template <int DT, int V>
+fs_status launch_d(const fs_format *f, const call &c)
+{
+    return c.d <= 32 ? launch_n<DT, V, 1>(f, c) : c.d <= 64 ? launch_n<DT, V, 2>(f, c) : launch_n<DT, V, 4>(f, c);
+}
+template <int DT>
+fs_status launch_v(const fs_format *f, const call &c)
+{
+    return f->V == 4 ? launch_d<DT, 4>(f, c) : f->V == 8 ? launch_d<DT, 8>(f, c) : launch_d<DT, 16>(f, c);
+}
+
+}  // namespace
+
+fs_status fs_zero_heads_launch(const fs_head_matrix *m, int64_t rows, int64_t columns, int heads, float *d_lse, hipStream_t st)
+{
+    if (rows == 0) return FS_OK;
+    const int64_t blocks = (rows * (columns / 8) + 255) / 256;
+    k_zero_heads<<<dim3((unsigned)blocks, heads), 256, 0, st>>>(fs_operand_of(m), rows, (int)(columns / 8), d_lse);
+    FS_LAUNCH_CHECK();
+    return FS_OK;
+}
+
+size_t fs_attention_forward_floats(const fs_format *f, int64_t heads, int64_t N)
+{
+    return fs_part_floats(f, heads, N + 2);  // the tiles, and a maximum and a sum per row
+}
+
+fs_status fs_attention_forward_launch(const fs_format *f, int heads, int kv_heads, int d, int N, float scale, const fs_head_matrix *X,
+                                      const fs_head_matrix *Y, const fs_head_matrix *H, const fs_bucket_bias *bias, const fs_dropout *drop,
+                                      const fs_head_matrix *out, float *lse, void *work, hipStream_t st)
+{
+    if (f->nvec == 0) return fs_zero_heads_launch(out, f->M, N, heads, lse, st);
+    const call c = {heads, heads / kv_heads, d, N, scale * 1.44269504088896340736f, fs_operand_of(X), fs_operand_of(Y), fs_operand_of(H), fs_operand_of(out),
+                    fs_bias_of(bias), fs_drop_of(drop), lse, (float *)work, st};
+    return f->dtype == FS_F16 ? launch_v<FS_F16>(f, c) : launch_v<FS_BF16>(f, c);
+}

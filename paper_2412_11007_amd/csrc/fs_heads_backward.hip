@@ -1,0 +1,433 @@
+// The gradients of attention with several heads, a bucket bias and dropout, in two walks that compute the scores again.
+//
+//   P = exp(s - lse),  D_i = g_i . out_i,  dS = P * (Z * (g_i . h_j) - D_i)
+//   by rows of A     dX_i = scale * sum_j dS y_j,  dtable[k] = sum of dS over bucket k
+//   by columns of A  dY_j = scale * sum_i dS x_i,  dH_j = sum_i Z P g_i          (rows of A^T, on its own format)
+//
+// Both walks are the forward pass's: per block of 32 vectors two operands are gathered (Y and H by rows, X and the gradient g of
+// out by columns), put to LDS, and used from there twice -- as they are against the window's rows in registers (scores and g . h,
+// contracted over the columns) and transposed against dS and Z P (the gradients, contracted over the vectors).  So a walk reads what
+// the forward pass reads, and nothing is kept of the scores; no atomics, since a walk's outputs belong to its windows.
+//
+// The walk by rows has lse and D per window row; it computes D when it meets the window and leaves {lse, D} per row and head
+// for the walk by columns, which gathers them beside the rows.  D comes from the rounded out: its error of half a step of the
+// element type in each product is of the size of the errors of Z P and dS, which are rounded for the matrix cores.  fp16 holds Z P scaled by
+// 2^12: probabilities are at most 1, and those of rows with thousands of entries would lie among its subnormal numbers.
+//
+// dtable: every lane adds the dS of its window row to a column of its own of a table of sums in LDS (V x 4 columns for each
+// bucket), a wavefront leaves one sum per bucket, and those are added in the order of the work list (fs_bucket_sums_launch).
+//
+// By columns the query heads that share keys and values are walked inside a block, one after the other, into the same accumulators.
+#include <type_traits>
+
+#include "fs_common.h"
+#include "fs_heads.h"
+
+namespace {
+
+template <int DT, int V, int KS, int NT>
+__global__ void __launch_bounds__(64)
+k_heads_rows(fs_walk a, fs_operand X, fs_operand Y, fs_operand H, fs_operand out, fs_operand G, const float *__restrict__ lse, int share, int d, int N,
+             float sl2, float scale, fs_bias_args bias, fs_drop_args drop, fs_operand dX, float2 *__restrict__ row_stats, float *__restrict__ part,
+             float *__restrict__ bucket_sums)
+{
+    using tile_y = fs_gathered<32 * KS>;
+    using tile_h = fs_gathered<16 * NT>;
+    constexpr int KN = NT / 2, COLS = 4 * V;
+    __shared__ __attribute__((aligned(16))) unsigned char lds_y[tile_y::kBytes];
+    __shared__ __attribute__((aligned(16))) unsigned char lds_h[tile_h::kBytes];
+    __shared__ __attribute__((aligned(16))) int lds_cols[32];
+    extern __shared__ __attribute__((aligned(16))) unsigned char dyn[];
+    float *table = reinterpret_cast<float *>(dyn);
+    uint8_t *lut = dyn + 4 * bias.n_buckets;
+    float *sums = reinterpret_cast<float *>(dyn + (fs_bias_lds_bytes(bias.n_buckets, bias.reach) + 15) / 16 * 16);
+
+    const int lane = threadIdx.x, head = blockIdx.y;
+    const int turn = __builtin_amdgcn_readfirstlane(fs_launch_turn<1>(blockIdx.x, a.slice, a.n_swz));
+    if (turn >= a.n_items) return;
+    const int4 it = a.items[turn];
+    const int nblk = it.y;
+    if (bucket_sums) {
+        bucket_sums += ((int64_t)head * a.n_items + turn) * bias.n_buckets;
+        if (nblk == 0) {
+            for (int i = lane; i < bias.n_buckets; i += 64) bucket_sums[i] = 0.f;
+            return;
+        }
+        for (int i = lane; i < bias.n_buckets * COLS; i += 64) sums[i] = 0.f;
+    }
+    if (nblk == 0) return;
+    int slot = it.z;
+    const int j = lane & 15, g = lane >> 4;
+    const int4 my_desc = a.blk_desc[it.x + min(lane, nblk - 1)];
+    auto block = [&](int i) -> BlockDesc { return fs_item_block(my_desc, i, nblk); };
+    const unsigned char *Xb = X.p + head * X.head, *Yb = Y.p + head / share * Y.head, *Hb = H.p + head / share * H.head;
+    const unsigned char *Gb = G.p + head * G.head, *Ob = out.p + head * out.head;
+    const uint32_t y_colb = tile_y::column_bytes(lane, d), h_colb = tile_h::column_bytes(lane, N);
+
+    BlockDesc d0 = block(0), d1 = block(1);
+    int cols0 = fs_block_cols(a, d0, lane), cols1 = fs_block_cols(a, d1, lane);
+    uint32_t bits0 = fs_lane_bits<V>(a, it.x, 0, nblk, lane);
+    // of the window: X's and g's rows, and lse (in units of log2) and D of row j
+    fs_frag xf[KS], gf[KN], of[KN];
+    float my_lse = 0.f;
+    auto load_window = [&](int w) {
+        fs_load_window<V>(xf, Xb, X.pitch, d, w, a.M, lane);
+        fs_load_window<V>(gf, Gb, G.pitch, N, w, a.M, lane);
+        fs_load_window<V>(of, Ob, out.pitch, N, w, a.M, lane);
+        const int64_t row = (int64_t)w * V + j;
+        my_lse = lse[(int64_t)head * a.M + (j < V && row < a.M ? row : 0)];
+    };
+    load_window(d0.w);
+    tile_y y;
+    tile_h h;
+    y.load(Yb, Y.pitch, y_colb, cols0, lane);
+    h.load(Hb, H.pitch, h_colb, cols0, lane);
+    if (bias.n_buckets > 0) {
+        fs_load_buckets(bias, lut, lane, 64);
+        for (int i = lane; i < bias.n_buckets; i += 64) table[i] = fs_widen<DT>(bias.table[head * bias.ld + i]) * 1.44269504088896340736f;
+    }
+    const fs_key key = fs_drop_key(drop, head);
+
+    fs_f4 acc[2 * KS];
+    fs_clear(acc);
+    bool from_first = d0.first, new_window = true;
+    float lse2 = 0.f, D = 0.f;
+    int step = 0;
+    auto block_step = [&](auto more_) {
+        constexpr bool MORE = decltype(more_)::value;
+        y.put(lds_y, lane, d);
+        h.put(lds_h, lane, N);
+        if (lane < 32) lds_cols[lane] = cols0;
+        const BlockDesc d2 = block(step + 2);
+        int cols2 = 0;
+        uint32_t bits1 = 0;
+        if constexpr (MORE) {
+            y.load(Yb, Y.pitch, y_colb, cols1, lane);
+            h.load(Hb, H.pitch, h_colb, cols1, lane);
+            cols2 = fs_block_cols(a, d2, lane);
+            bits1 = fs_lane_bits<V>(a, it.x, step + 1, nblk, lane);
+        }
+        const int row = d0.w * V + j;
+        if (new_window) {
+            D = 0.f;
+#pragma unroll
+            for (int ks = 0; ks < KN; ks++)
+#pragma unroll
+                for (int k = 0; k < 8; k++) D = fmaf(fs_widen<DT>(gf[ks].e[k]), fs_widen<DT>(of[ks].e[k]), D);
+            D += __shfl_xor(D, 16, 64);
+            D += __shfl_xor(D, 32, 64);
+            // a row of which nothing is left: exp(s - lse) has to come out as zero
+            lse2 = my_lse == -INFINITY ? INFINITY : my_lse * 1.44269504088896340736f;
+            if (d0.first && g == 0 && j < V && row < a.M) row_stats[(int64_t)head * a.M + row] = make_float2(lse2, D);
+        }
+        FS_WAVE_SYNC();
+        fs_f4 sc[2], gp[2];
+#pragma unroll
+        for (int t = 0; t < 2; t++) {
+            sc[t] = tile_y::template contract<DT>(lds_y, t, lane, xf);
+            gp[t] = tile_h::template contract<DT>(lds_h, t, lane, gf);
+        }
+        uint32_t kept = bits0;
+        if (drop.state) kept = fs_kept(bits0, key, drop.below, [&](int x) -> int2 { return make_int2(row, lds_cols[8 * g + x]); });
+        float ds[8];
+#pragma unroll
+        for (int x = 0; x < 8; x++) {
+            float t = sc[x >> 2][x & 3] * sl2;
+            int b = 0;
+            if (bias.n_buckets > 0) {
+                b = fs_bucket_of(lut, bias.reach, bias.shift, row, lds_cols[8 * g + x]);
+                t += table[b];
+            }
+            const float p = __builtin_amdgcn_exp2f(t - lse2);
+            const float gz = kept >> x & 1u ? gp[x >> 2][x & 3] * drop.factor : 0.f;
+            ds[x] = bits0 >> x & 1u ? p * (gz - D) : 0.f;
+            if (bucket_sums && (bits0 >> x & 1u)) fs_lds_add(sums + COLS * b + g * V + j, ds[x]);
+        }
+        const fs_frag sp = fs_round8<DT>(ds);
+        if (d0.kb > 0) {
+#pragma unroll
+            for (int t = 0; t < 2 * KS; t++) acc[t] = fs_mfma_16x16x32<DT>(tile_y::transposed(lds_y, t, lane), sp, acc[t]);
+        }
+        FS_WAVE_SYNC();
+        new_window = MORE && d1.w != d0.w;
+        if (new_window) load_window(d1.w);
+        if (d0.last || !MORE) {
+            if (d0.last && from_first) {
+                fs_store_window<DT, V, 32 * KS>(lds_y, acc, scale, dX.p + head * dX.head, dX.pitch, d, d0.w, a.M, lane);
+            } else {
+                fs_store_part<V>(part + (int64_t)head * a.n_slots * V * d, slot, d, acc, lane);
+                slot++;
+            }
+            fs_clear(acc);
+        }
+        if (d0.last) from_first = true;
+        d0 = d1;
+        d1 = d2;
+        cols0 = cols1;
+        cols1 = cols2;
+        bits0 = bits1;
+    };
+    for (; step + 1 < nblk; step++) block_step(std::true_type{});
+    block_step(std::false_type{});
+    if (bucket_sums) {
+        FS_WAVE_SYNC();
+        fs_store_bucket_sums<COLS>(sums, bias.n_buckets, lane, bucket_sums);
+    }
+}
+
+// By columns: `a` walks A^T, its vectors are rows of A (`rows` of them) and its window rows columns.
+template <int DT, int V, int KS, int NT>
+__global__ void __launch_bounds__(64)
+k_heads_cols(fs_walk a, int64_t rows, fs_operand X, fs_operand Y, fs_operand H, fs_operand G, const float2 *__restrict__ row_stats, int share, int d,
+             int N, float sl2, float scale, fs_bias_args bias, fs_drop_args drop, fs_operand dY, fs_operand dH, float *__restrict__ part_y,
+             float *__restrict__ part_h)
+{
+    using tile_x = fs_gathered<32 * KS>;
+    using tile_g = fs_gathered<16 * NT>;
+    constexpr int KN = NT / 2;
+    constexpr float kWeight = DT == FS_F16 ? 4096.f : 1.f;
+    __shared__ __attribute__((aligned(16))) unsigned char lds_x[tile_x::kBytes];
+    __shared__ __attribute__((aligned(16))) unsigned char lds_g[tile_g::kBytes];
+    __shared__ __attribute__((aligned(16))) int lds_rows[32];
+    __shared__ __attribute__((aligned(16))) float2 lds_stats[32];
+    extern __shared__ __attribute__((aligned(16))) unsigned char dyn[];
+    float *table = reinterpret_cast<float *>(dyn);  // of `share` heads
+    uint8_t *lut = dyn + 4 * bias.n_buckets * share;
+
+    const int lane = threadIdx.x, kv = blockIdx.y;
+    const int turn = __builtin_amdgcn_readfirstlane(fs_launch_turn<1>(blockIdx.x, a.slice, a.n_swz));
+    if (turn >= a.n_items) return;
+    const int4 it = a.items[turn];
+    const int nblk = it.y;
+    if (nblk == 0) return;
+    int slot = it.z;
+    const int j = lane & 15, g = lane >> 4;
+    const int4 my_desc = a.blk_desc[it.x + min(lane, nblk - 1)];
+    auto block = [&](int i) -> BlockDesc { return fs_item_block(my_desc, i, nblk); };
+    const unsigned char *Yb = Y.p + kv * Y.head, *Hb = H.p + kv * H.head;
+    const uint32_t x_colb = tile_x::column_bytes(lane, d), g_colb = tile_g::column_bytes(lane, N);
+
+    tile_x x_;
+    tile_g g_;
+    float2 st;
+    auto gather = [&](int member, int row_of_lane) {  // of query head kv * share + member
+        const int head = kv * share + member;
+        x_.load(X.p + head * X.head, X.pitch, x_colb, row_of_lane, lane);
+        g_.load(G.p + head * G.head, G.pitch, g_colb, row_of_lane, lane);
+        st = row_stats[head * rows + row_of_lane];
+    };
+    BlockDesc d0 = block(0), d1 = block(1);
+    int rows0 = fs_block_cols(a, d0, lane), rows1 = fs_block_cols(a, d1, lane);
+    uint32_t bits0 = fs_lane_bits<V>(a, it.x, 0, nblk, lane), bits1 = fs_lane_bits<V>(a, it.x, 1, nblk, lane);
+    fs_frag yf[KS], hf[KN];
+    fs_load_window<V>(yf, Yb, Y.pitch, d, d0.w, a.M, lane);
+    fs_load_window<V>(hf, Hb, H.pitch, N, d0.w, a.M, lane);
+    gather(0, rows0);
+    if (bias.n_buckets > 0) {
+        fs_load_buckets(bias, lut, lane, 64);
+        for (int i = lane; i < bias.n_buckets * share; i += 64)
+            table[i] = fs_widen<DT>(bias.table[(kv * share + i / bias.n_buckets) * bias.ld + i % bias.n_buckets]) * 1.44269504088896340736f;
+    }
+    fs_key keys = fs_key{0u, 0u};  // lane i: that of the group's head i
+    if (drop.state) {
+        const uint64_t seed = (uint64_t)drop.state[0], at = (uint64_t)drop.state[1];
+        keys = fs_threefry<20>(fs_key{(uint32_t)seed, (uint32_t)(seed >> 32)}, (uint32_t)at, (uint32_t)(at >> 32));
+        keys = fs_threefry<20>(keys, (uint32_t)(kv * share + lane), 0u);
+    }
+
+    fs_f4 acc_y[2 * KS], acc_h[NT];
+    fs_clear(acc_y);
+    fs_clear(acc_h);
+    bool from_first = d0.first;
+    int step = 0, member = 0;
+    for (;;) {  // a head of a block at a time
+        const bool block_done = member + 1 == share, done = block_done && step + 1 == nblk;
+        x_.put(lds_x, lane, d);
+        g_.put(lds_g, lane, N);
+        if (lane < 32) {
+            lds_rows[lane] = rows0;
+            lds_stats[lane] = st;
+        }
+        BlockDesc d2 = d1;
+        int rows2 = rows1;
+        uint32_t bits2 = bits1;
+        gather(block_done ? 0 : member + 1, block_done ? rows1 : rows0);  // (behind the last block: its own rows once more)
+        if (block_done) {
+            d2 = block(step + 2);
+            rows2 = fs_block_cols(a, d2, lane);
+            bits2 = fs_lane_bits<V>(a, it.x, step + 2, nblk, lane);
+        }
+        FS_WAVE_SYNC();
+        fs_f4 sc[2], gp[2];
+#pragma unroll
+        for (int t = 0; t < 2; t++) {
+            sc[t] = tile_x::template contract<DT>(lds_x, t, lane, yf);
+            gp[t] = tile_g::template contract<DT>(lds_g, t, lane, hf);
+        }
+        const int col = d0.w * V + j;
+        uint32_t kept = bits0;
+        if (drop.state) {
+            const fs_key key = fs_key{(uint32_t)__builtin_amdgcn_readlane((int)keys.k0, member), (uint32_t)__builtin_amdgcn_readlane((int)keys.k1, member)};
+            kept = fs_kept(bits0, key, drop.below, [&](int x) -> int2 { return make_int2(lds_rows[8 * g + x], col); });
+        }
+        float ds[8], w[8];
+#pragma unroll
+        for (int x = 0; x < 8; x++) {
+            float t = sc[x >> 2][x & 3] * sl2;
+            if (bias.n_buckets > 0) t += table[member * bias.n_buckets + fs_bucket_of(lut, bias.reach, bias.shift, lds_rows[8 * g + x], col)];
+            const float2 rs = lds_stats[8 * g + x];
+            const float p = __builtin_amdgcn_exp2f(t - rs.x);
+            const bool keep = kept >> x & 1u;
+            w[x] = keep ? p * kWeight : 0.f;
+            ds[x] = bits0 >> x & 1u ? p * ((keep ? gp[x >> 2][x & 3] * drop.factor : 0.f) - rs.y) : 0.f;
+        }
+        const fs_frag sy = fs_round8<DT>(ds), sh = fs_round8<DT>(w);
+        if (d0.kb > 0) {
+#pragma unroll
+            for (int t = 0; t < 2 * KS; t++) acc_y[t] = fs_mfma_16x16x32<DT>(tile_x::transposed(lds_x, t, lane), sy, acc_y[t]);
+#pragma unroll
+            for (int t = 0; t < NT; t++) acc_h[t] = fs_mfma_16x16x32<DT>(tile_g::transposed(lds_g, t, lane), sh, acc_h[t]);
+        }
+        FS_WAVE_SYNC();
+        if (!block_done) {
+            member++;
+            continue;
+        }
+        member = 0;
+        if (!done && d1.w != d0.w) {
+            fs_load_window<V>(yf, Yb, Y.pitch, d, d1.w, a.M, lane);
+            fs_load_window<V>(hf, Hb, H.pitch, N, d1.w, a.M, lane);
+        }
+        if (d0.last || done) {
+            if (d0.last && from_first) {
+                fs_store_window<DT, V, 32 * KS>(lds_x, acc_y, scale, dY.p + kv * dY.head, dY.pitch, d, d0.w, a.M, lane);
+                fs_store_window<DT, V, 16 * NT>(lds_g, acc_h, drop.factor / kWeight, dH.p + kv * dH.head, dH.pitch, N, d0.w, a.M, lane);
+            } else {
+                fs_store_part<V>(part_y + (int64_t)kv * a.n_slots * V * d, slot, d, acc_y, lane);
+                fs_store_part<V>(part_h + (int64_t)kv * a.n_slots * V * N, slot, N, acc_h, lane);
+                slot++;
+            }
+            fs_clear(acc_y);
+            fs_clear(acc_h);
+        }
+        if (done) break;
+        if (d0.last) from_first = true;
+        step++;
+        d0 = d1;
+        d1 = d2;
+        rows0 = rows1;
+        rows1 = rows2;
+        bits0 = bits1;
+        bits1 = bits2;
+    }
+}
+
+struct call {
+    int heads, kv_heads, d, N, n_grad;  // n_grad: buckets whose gradient is asked for, or 0
+    float scale;
+    fs_operand X, Y, H, out, G, dX, dY, dH;
+    const float *lse;
+    void *table_grad;
+    fs_bias_args bias;
+    fs_drop_args drop;
+    float *work;
+    hipStream_t st;
+};
+
+template <int DT, int V>
+fs_status add_parts(const fs_format *f, int heads, const float *part, int columns, const fs_operand &to, float factor, hipStream_t st)
+{
+    if (f->n_split_windows == 0) return FS_OK;
+    const int64_t blocks = f->n_split_windows * ((columns + 31) / 32);
+    if (blocks >= ((int64_t)1 << 31)) return FS_ERR_TOO_LARGE;
+    k_add_parts<DT, V, false><<<dim3((unsigned)blocks, heads), 64, 0, st>>>((const int4 *)f->split_windows, part, nullptr, (int)f->n_split_items, columns, to, factor,
+                                                                          f->M, nullptr);
+    FS_LAUNCH_CHECK();
+    return FS_OK;
+}
+
+// Where the workspace's pieces lie, in floats: {lse, D} per row and head, the buckets' sums, the partial tiles of the walk in progress.
+struct pieces {
+    size_t sums, tiles, total;
+};
+pieces pieces_of(const fs_format *f, const fs_format *t, int64_t heads, int64_t kv_heads, int64_t d, int64_t N, int64_t n_grad)
+{
+    pieces p;
+    p.sums = fs_align_up(2 * (size_t)heads * (size_t)f->M, 4);
+    p.tiles = p.sums + fs_align_up(n_grad > 0 ? fs_bucket_sums_floats(heads, f->n_items, n_grad) : 0, 4);
+    p.total = p.tiles + std::max(fs_part_floats(f, heads, d), fs_part_floats(t, kv_heads, d + N));
+    return p;
+}
+
+template <int DT, int V, int KS, int NT>
+fs_status rows_launch(const fs_format *f, const call &c, const pieces &at)
+{
+    const fs_launch_geometry geo = fs_launch_geometry_for(f, 1);
+    float *tiles = c.work + at.tiles, *sums = c.n_grad > 0 ? c.work + at.sums : nullptr;
+    const size_t lds = (fs_bias_lds_bytes(c.bias.n_buckets, c.bias.reach) + 15) / 16 * 16 + (size_t)c.n_grad * 16 * V;
+    k_heads_rows<DT, V, KS, NT><<<dim3(geo.nbx, c.heads), 64, lds, c.st>>>(fs_walk_of(f, geo), c.X, c.Y, c.H, c.out, c.G, c.lse, c.heads / c.kv_heads, c.d, c.N,
+                                                                          c.scale * 1.44269504088896340736f, c.scale, c.bias, c.drop, c.dX, (float2 *)c.work, tiles, sums);
+    FS_LAUNCH_CHECK();
+    const fs_status s = add_parts<DT, V>(f, c.heads, tiles, c.d, c.dX, c.scale, c.st);
+    return s != FS_OK || !sums ? s : fs_bucket_sums_launch(DT, c.heads, (int)f->n_items, c.n_grad, sums, c.table_grad, c.st);
+}
+
+template <int DT, int V, int KS, int NT>
+fs_status cols_launch(const fs_format *f, const fs_format *t, const call &c, const pieces &at)
+{
+    const fs_launch_geometry geo = fs_launch_geometry_for(t, 1);
+    const int share = c.heads / c.kv_heads;
+    float *tiles_y = c.work + at.tiles, *tiles_h = tiles_y + fs_part_floats(t, c.kv_heads, c.d);
+    const size_t lds = c.bias.n_buckets > 0 ? fs_bias_lds_bytes(c.bias.n_buckets, c.bias.reach) + 4 * (size_t)c.bias.n_buckets * (share - 1) : 0;
+    k_heads_cols<DT, V, KS, NT><<<dim3(geo.nbx, c.kv_heads), 64, lds, c.st>>>(fs_walk_of(t, geo), f->M, c.X, c.Y, c.H, c.G, (const float2 *)c.work, share, c.d, c.N,
+                                                                             c.scale * 1.44269504088896340736f, c.scale, c.bias, c.drop, c.dY, c.dH, tiles_y, tiles_h);
+    FS_LAUNCH_CHECK();
+    const fs_status s = add_parts<DT, V>(t, c.kv_heads, tiles_y, c.d, c.dY, c.scale, c.st);
+    return s != FS_OK ? s : add_parts<DT, V>(t, c.kv_heads, tiles_h, c.N, c.dH, c.drop.factor * (DT == FS_F16 ? 1.f / 4096.f : 1.f), c.st);
+}
+
+// The two formats may have windows of different heights.
+template <int DT, int KS, int NT>
+fs_status launch(const fs_format *f, const fs_format *t, const call &c)
+{
+    const pieces at = pieces_of(f, t, c.heads, c.kv_heads, c.d, c.N, c.n_grad);
+    const fs_status s = f->V == 4   ? rows_launch<DT, 4, KS, NT>(f, c, at)
+                        : f->V == 8 ? rows_launch<DT, 8, KS, NT>(f, c, at)
+                                    : rows_launch<DT, 16, KS, NT>(f, c, at);
+    if (s != FS_OK) return s;
+    return t->V == 4 ? cols_launch<DT, 4, KS, NT>(f, t, c, at) : t->V == 8 ? cols_launch<DT, 8, KS, NT>(f, t, c, at) : cols_launch<DT, 16, KS, NT>(f, t, c, at);
+}
+template <int DT, int KS>
+fs_status launch_n(const fs_format *f, const fs_format *t, const call &c)
+{
+    return c.N <= 32 ? launch<DT, KS, 2>(f, t, c) : c.N <= 64 ? launch<DT, KS, 4>(f, t, c) : launch<DT, KS, 8>(f, t, c);
+}
+template <int DT>
+fs_status launch_d(const fs_format *f, const fs_format *t, const call &c)
+{
+    return c.d <= 32 ? launch_n<DT, 1>(f, t, c) : c.d <= 64 ? launch_n<DT, 2>(f, t, c) : launch_n<DT, 4>(f, t, c);
+}
+
+}  // namespace
+
+size_t fs_attention_backward_floats(const fs_format *f, const fs_format *t, int64_t heads, int64_t kv_heads, int64_t d, int64_t N, int64_t n_grad)
+{
+    return pieces_of(f, t, heads, kv_heads, d, N, n_grad).total;
+}
+
+fs_status fs_attention_backward_launch(const fs_format *f, const fs_format *t, int heads, int kv_heads, int d, int N, float scale, const fs_head_matrix *X,
+                                       const fs_head_matrix *Y, const fs_head_matrix *H, const fs_bucket_bias *bias, const fs_dropout *drop,
+                                       const fs_head_matrix *out, const float *lse, const fs_head_matrix *G, const fs_head_matrix *dX,
+                                       const fs_head_matrix *dY, const fs_head_matrix *dH, void *table_grad, void *work, hipStream_t st)
+{
+    if (f->nvec == 0) {
+        fs_status s = fs_zero_heads_launch(dX, f->M, d, heads, nullptr, st);
+        if (s == FS_OK) s = fs_zero_heads_launch(dY, f->K, d, kv_heads, nullptr, st);
+        if (s == FS_OK) s = fs_zero_heads_launch(dH, f->K, N, kv_heads, nullptr, st);
+        return s != FS_OK || !table_grad ? s : fs_bucket_sums_launch(f->dtype, heads, 0, bias->n_buckets, (float *)work, table_grad, st);
+    }
+    const call c = {heads, kv_heads, d, N, table_grad ? bias->n_buckets : 0, scale,
+                    fs_operand_of(X), fs_operand_of(Y), fs_operand_of(H), fs_operand_of(out), fs_operand_of(G), fs_operand_of(dX), fs_operand_of(dY), fs_operand_of(dH),
+                    lse, table_grad, fs_bias_of(bias), fs_drop_of(drop), (float *)work, st};
+    return f->dtype == FS_F16 ? launch_d<FS_F16>(f, t, c) : launch_d<FS_BF16>(f, t, c);
+}
