@@ -13,9 +13,10 @@ CALLS_SRC = os.path.join(_HERE, "csrc", "fs_torch.cpp")
 CALLS_LIB = os.path.join(_HERE, "_fs_torch.so")
 OBJ_DIR = os.path.join(_HERE, "_build")  # object files; ignored by git
 # k_sddmm uses its matrix-core results at once: let them land in ordinary vector registers instead of
-# accumulation registers that eight copy instructions per block would have to read back (the other kernels
-# get this form from the compiler unasked)
-FILE_FLAGS = {"fs_sddmm.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
+# accumulation registers that eight copy instructions per block would have to read back; the kernels with heads use theirs
+# at once as well, or scale them every block (the other kernels get this form from the compiler unasked)
+VGPR_FORM = ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]
+FILE_FLAGS = {"fs_sddmm.hip": VGPR_FORM, "fs_heads.hip": VGPR_FORM, "fs_heads_backward.hip": VGPR_FORM}
 
 
 def _run(cmd, verbose):

@@ -103,7 +103,7 @@ k_edges(const int4 *__restrict__ blk_desc, int n_blocks, const uint32_t *__restr
                     const int r = row_of(k);
                     const int b = fs_bucket_of(lut, bias.reach, bias.shift, row0 + r, cols[e0 + k - r * kb]);
                     if constexpr (OP == OP_BIAS) y[k] = fmaf(scale, fs_widen<DT>(v.e[k]), table[b]);
-                    else fs_lds_add(mine + 64 * b, fs_widen<DT>(v.e[k]));
+                    else mine[64 * b] += fs_widen<DT>(v.e[k]);
                 }
             }
             if constexpr (OP == OP_BIAS) v.u = fs_u4{fs_pack2<DT>(y[0], y[1]), fs_pack2<DT>(y[2], y[3]), fs_pack2<DT>(y[4], y[5]), fs_pack2<DT>(y[6], y[7])};

@@ -139,6 +139,13 @@ __device__ __forceinline__ float fs_log_sum(float m, float l)
     return l == 0.f ? -INFINITY : 0.693147180559945309f * (m + __builtin_amdgcn_logf(l));
 }
 
+// A bias in units of log2, its lowest bit free for a flag (fs_entries).
+__device__ __forceinline__ float fs_flagless_log2(float b)
+{
+    const float t = b * 1.44269504088896340736f;
+    return t != t ? t : __uint_as_float(__float_as_uint(t) & ~1u);
+}
+
 // Host side: the checked arguments as the kernels take them.
 inline fs_bias_args fs_bias_of(const fs_bucket_bias *b)
 {
@@ -214,10 +221,15 @@ struct fs_gathered {
     static __device__ __forceinline__ uint32_t column_bytes(int lane, int width) { return 2 * (uint32_t)min((lane % LPR) * 8, width - 8); }
     __device__ __forceinline__ void put(unsigned char *lds, int lane, int width) const
     {
-        const bool in = (lane % LPR) * 8 < width;
         unsigned char *to = lds + lds_row<RS>(lane / LPR) + (lane % LPR) * 16;
+        if (width == NC) {
 #pragma unroll
-        for (int l = 0; l < NLD; l++) *reinterpret_cast<fs_u4 *>(to + lds_row<RS>(l * RPI)) = in ? r[l] : fs_u4{0u, 0u, 0u, 0u};
+            for (int l = 0; l < NLD; l++) *reinterpret_cast<fs_u4 *>(to + lds_row<RS>(l * RPI)) = r[l];
+        } else {
+            const bool in = (lane % LPR) * 8 < width;
+#pragma unroll
+            for (int l = 0; l < NLD; l++) *reinterpret_cast<fs_u4 *>(to + lds_row<RS>(l * RPI)) = in ? r[l] : fs_u4{0u, 0u, 0u, 0u};
+        }
     }
     // tile t of the products with an operand held in registers: lane (j, g) gets vectors 8g + 4t .. +3 of window row j
     template <int DT, int STEPS>
@@ -270,14 +282,121 @@ __device__ __forceinline__ int fs_block_cols(const fs_walk &a, const BlockDesc &
     return a.vec_col[max(min(b.s + min(lane & 31, b.kb - 1), a.nvec - 1), 0)];
 }
 
-// Occupancy of window row j in block i of an item: the eight vectors 8g .. 8g+7 of the lane (none for lanes past V).
+// Occupancy of window row j in block i of an item: bit c, the row stores the block's vector c (none for lanes past V).
 template <int V>
-__device__ __forceinline__ uint32_t fs_lane_bits(const fs_walk &a, int first_slot, int i, int nblk, int lane)
+__device__ __forceinline__ uint32_t fs_row_bits(const fs_walk &a, int first_slot, int i, int nblk, int lane)
 {
-    const int j = lane & 15, g = lane >> 4;
+    const int j = lane & 15;
     const uint32_t m = a.row_bits[(int64_t)(first_slot + min(i, nblk - 1)) * V + (j & (V - 1))];
-    return i < nblk && j < V ? m >> (8 * g) & 255u : 0u;
+    return i < nblk && j < V ? m : 0u;
 }
+
+// What an entry needs beside its score -- a bias from its bucket, a word of the generator -- takes about 70 instructions.  In the
+// scores' layout a lane has eight places, and taken place by place they were most of a block's: of a power-law graph an eighth of
+// the places are stored, and with eight rows a window half the lanes have none.  So every lane takes one entry at a time from a list in LDS
+// or, where more than half of the block is stored, one place at a time in row order, without a list.  The results go to `value`, a
+// V x 32 tile of biases whose lowest bit says whether dropout keeps the entry (of the 24 bits of a mantissa, for a bias of 8 or 11).
+template <int V>
+struct fs_entries {
+    static constexpr int kPitch = 36;  // floats from a row of `value` to the next: rows start in different banks
+    uint16_t list[32 * V];             // vector | row << 5 | bucket << 9
+    float value[V * kPitch] __attribute__((aligned(16)));
+
+    // m: occupancy of row j.  Returns how many of the list's elements to take, the same in all lanes.
+    __device__ __forceinline__ int make_list(uint32_t m, int lane)
+    {
+        const int j = lane & 15, g = lane >> 4;
+        const int own = __popc(m);
+        int sum = own;  // over the rows up to j
+        sum += __builtin_amdgcn_update_dpp(0, sum, 0x111, 0xF, 0xF, true);  // row_shr:1
+        sum += __builtin_amdgcn_update_dpp(0, sum, 0x112, 0xF, 0xF, true);
+        sum += __builtin_amdgcn_update_dpp(0, sum, 0x114, 0xF, 0xF, true);
+        sum += __builtin_amdgcn_update_dpp(0, sum, 0x118, 0xF, 0xF, true);
+        const int n = __builtin_amdgcn_readlane(sum, 15);
+        if (n > 16 * V) return 32 * V;
+        int at = sum - own + __popc(m & ((1u << (8 * g)) - 1u));
+        for (uint32_t m8 = m >> (8 * g) & 255u; m8; m8 &= m8 - 1) list[at++] = (uint16_t)(8 * g + __builtin_ctz(m8) | j << 5);
+        return n;
+    }
+    // T: window rows are columns of A.  cols: lane l holds the column (T: row) of vector l mod 32; lds_cols the same in LDS.
+    template <bool T>
+    __device__ __forceinline__ void look_up(int n, int lane, int row0, int cols, const int *lds_cols, const fs_bias_args &b, const float *table,
+                                            const uint8_t *lut, const fs_drop_args &drop, fs_key key)
+    {
+        auto bucket = [&](int j, int col) -> int { return fs_bucket_of(lut, b.reach, b.shift, T ? col : row0 + j, T ? row0 + j : col); };
+        auto keep = [&](int j, int col) -> uint32_t {
+            return fs_threefry<13>(key, (uint32_t)(T ? col : row0 + j), (uint32_t)(T ? row0 + j : col)).k0 >= drop.below ? 1u : 0u;
+        };
+        auto with = [](float bias, uint32_t kept) -> float {  // (infinities stay what they are)
+            const uint32_t v = __float_as_uint(bias);
+            return __uint_as_float((v & 0x7F800000u) == 0x7F800000u ? v : v | kept);
+        };
+        if (n == 32 * V) {
+            const int c = lane & 31, j0 = lane >> 5;
+            constexpr int P = V / 2 < 4 ? V / 2 : 4;  // side by side
+#pragma unroll
+            for (int i0 = 0; i0 < V / 2; i0 += P) {
+                float v[P];
+                if (b.n_buckets > 0) {
+                    int k[P];
+#pragma unroll
+                    for (int i = 0; i < P; i++) k[i] = bucket(2 * (i0 + i) + j0, cols);
+#pragma unroll
+                    for (int i = 0; i < P; i++) {
+                        v[i] = table[k[i]];
+                        list[64 * (i0 + i) + lane] = (uint16_t)(64 * (i0 + i) + lane | k[i] << 9);
+                    }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < P; i++) v[i] = 0.f;
+                }
+                if (drop.state) {
+#pragma unroll
+                    for (int i = 0; i < P; i++) v[i] = with(v[i], keep(2 * (i0 + i) + j0, cols));
+                }
+#pragma unroll
+                for (int i = 0; i < P; i++) value[(2 * (i0 + i) + j0) * kPitch + c] = v[i];
+            }
+        } else {
+            FS_WAVE_SYNC();
+            for (int r = lane; r < n; r += 64) {
+                const int code = list[r] & 511, c = code & 31, j = code >> 5;
+                const int col = lds_cols[c];
+                float v = 0.f;
+                if (b.n_buckets > 0) {
+                    const int k = bucket(j, col);
+                    v = table[k];
+                    list[r] = (uint16_t)(code | k << 9);
+                }
+                if (drop.state) v = with(v, keep(j, col));
+                value[j * kPitch + c] = v;
+            }
+        }
+        FS_WAVE_SYNC();
+    }
+    // of the lane's places: row j, vectors 8g .. 8g+7
+    __device__ __forceinline__ void values(float (&v)[8], int lane) const
+    {
+        const fs_f4 *from = reinterpret_cast<const fs_f4 *>(value + (lane & (V - 1)) * kPitch + 8 * (lane >> 4));
+        const fs_f4 lo = from[0], hi = from[1];
+#pragma unroll
+        for (int x = 0; x < 4; x++) {
+            v[x] = lo[x];
+            v[4 + x] = hi[x];
+        }
+    }
+    __device__ __forceinline__ void put_values(const float (&v)[8], int lane)
+    {
+        if ((lane & 15) >= V) return;
+        fs_f4 *to = reinterpret_cast<fs_f4 *>(value + (lane & 15) * kPitch + 8 * (lane >> 4));
+        to[0] = fs_f4{v[0], v[1], v[2], v[3]};
+        to[1] = fs_f4{v[4], v[5], v[6], v[7]};
+    }
+};
+
+// Bit x of m as 0 or ~0, and a choice by it.
+__device__ __forceinline__ uint32_t fs_bit_mask(uint32_t m, int x) { return (uint32_t)__builtin_amdgcn_sbfe((int)m, x, 1); }
+__device__ __forceinline__ float fs_choose(uint32_t mask, float a, float b) { return __uint_as_float((mask & __float_as_uint(a)) | (~mask & __float_as_uint(b))); }
 
 template <int NT>
 __device__ __forceinline__ void fs_clear(fs_f4 (&acc)[NT])

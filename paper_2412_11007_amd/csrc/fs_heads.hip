@@ -30,6 +30,7 @@ k_heads_forward(fs_walk a, fs_operand X, fs_operand Y, fs_operand H, int share, 
     __shared__ __attribute__((aligned(16))) unsigned char lds_y[tile_y::kBytes];
     __shared__ __attribute__((aligned(16))) unsigned char lds_h[tile_h::kBytes];
     __shared__ __attribute__((aligned(16))) int lds_cols[32];
+    __shared__ fs_entries<V> entries;
     extern __shared__ __attribute__((aligned(16))) unsigned char dyn[];
     float *table = reinterpret_cast<float *>(dyn);
     uint8_t *lut = dyn + 4 * bias.n_buckets;
@@ -49,7 +50,7 @@ k_heads_forward(fs_walk a, fs_operand X, fs_operand Y, fs_operand H, int share, 
 
     BlockDesc d0 = block(0), d1 = block(1);
     int cols0 = fs_block_cols(a, d0, lane), cols1 = fs_block_cols(a, d1, lane);
-    uint32_t bits0 = fs_lane_bits<V>(a, it.x, 0, nblk, lane);
+    uint32_t bits0 = fs_row_bits<V>(a, it.x, 0, nblk, lane);
     fs_frag xf[KS];
     fs_load_window<V>(xf, Xb, X.pitch, d, d0.w, a.M, lane);
     tile_y y;
@@ -58,9 +59,11 @@ k_heads_forward(fs_walk a, fs_operand X, fs_operand Y, fs_operand H, int share, 
     h.load(Hb, H.pitch, h_colb, cols0, lane);
     if (bias.n_buckets > 0) {
         fs_load_buckets(bias, lut, lane, 64);
-        for (int i = lane; i < bias.n_buckets; i += 64) table[i] = fs_widen<DT>(bias.table[head * bias.ld + i]) * 1.44269504088896340736f;
+        for (int i = lane; i < bias.n_buckets; i += 64) table[i] = fs_flagless_log2(fs_widen<DT>(bias.table[head * bias.ld + i]));
     }
     const fs_key key = fs_drop_key(drop, head);
+
+    const bool looks_up = bias.n_buckets > 0 || drop.state;
 
     fs_f4 acc[NT];
     fs_clear(acc);
@@ -79,19 +82,34 @@ k_heads_forward(fs_walk a, fs_operand X, fs_operand Y, fs_operand H, int share, 
             y.load(Yb, Y.pitch, y_colb, cols1, lane);
             h.load(Hb, H.pitch, h_colb, cols1, lane);
             cols2 = fs_block_cols(a, d2, lane);
-            bits1 = fs_lane_bits<V>(a, it.x, step + 1, nblk, lane);
+            bits1 = fs_row_bits<V>(a, it.x, step + 1, nblk, lane);
         }
         FS_WAVE_SYNC();
+        if (looks_up) entries.template look_up<false>(entries.make_list(bits0, lane), lane, d0.w * V, cols0, lds_cols, bias, table, lut, drop, key);
         fs_f4 sc[2];
 #pragma unroll
         for (int t = 0; t < 2; t++) sc[t] = tile_y::template contract<DT>(lds_y, t, lane, xf);
         const int row = d0.w * V + j;
+        const uint32_t m8 = bits0 >> (8 * g);
         float p[8], mx = -INFINITY;
+        uint32_t kept[8];
+        if (looks_up) {
+            entries.values(p, lane);
+#pragma unroll
+            for (int x = 0; x < 8; x++) {
+                kept[x] = drop.state ? fs_bit_mask(__float_as_uint(p[x]), 0) : ~0u;
+                p[x] = fmaf(sc[x >> 2][x & 3], sl2, p[x]);
+            }
+        } else {
+#pragma unroll
+            for (int x = 0; x < 8; x++) {
+                kept[x] = ~0u;
+                p[x] = sc[x >> 2][x & 3] * sl2;
+            }
+        }
 #pragma unroll
         for (int x = 0; x < 8; x++) {
-            float t = sc[x >> 2][x & 3] * sl2;
-            if (bias.n_buckets > 0) t += table[fs_bucket_of(lut, bias.reach, bias.shift, row, lds_cols[8 * g + x])];
-            p[x] = bits0 >> x & 1u ? t : -INFINITY;
+            p[x] = fs_choose(fs_bit_mask(m8, x), p[x], -INFINITY);
             mx = fmaxf(mx, p[x]);
         }
         mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
@@ -107,11 +125,8 @@ k_heads_forward(fs_walk a, fs_operand X, fs_operand Y, fs_operand H, int share, 
         }
         l_run = l_run * corr + ps;
         m_run = m_new;
-        if (drop.state) {
-            const uint32_t kept = fs_kept(bits0, key, drop.below, [&](int x) -> int2 { return make_int2(row, lds_cols[8 * g + x]); });
 #pragma unroll
-            for (int x = 0; x < 8; x++) p[x] = kept >> x & 1u ? p[x] : 0.f;
-        }
+        for (int x = 0; x < 8; x++) p[x] = __uint_as_float(kept[x] & __float_as_uint(p[x]));
         const fs_frag sp = fs_round8<DT>(p);
         if (d0.kb > 0) {
 #pragma unroll

@@ -25,6 +25,8 @@
 
 namespace {
 
+constexpr int kSumColumns = 32;  // of the table of sums in LDS, for each bucket
+
 template <int DT, int V, int KS, int NT>
 __global__ void __launch_bounds__(64)
 k_heads_rows(fs_walk a, fs_operand X, fs_operand Y, fs_operand H, fs_operand out, fs_operand G, const float *__restrict__ lse, int share, int d, int N,
@@ -33,10 +35,11 @@ k_heads_rows(fs_walk a, fs_operand X, fs_operand Y, fs_operand H, fs_operand out
 {
     using tile_y = fs_gathered<32 * KS>;
     using tile_h = fs_gathered<16 * NT>;
-    constexpr int KN = NT / 2, COLS = 4 * V;
+    constexpr int KN = NT / 2, COLS = kSumColumns;
     __shared__ __attribute__((aligned(16))) unsigned char lds_y[tile_y::kBytes];
     __shared__ __attribute__((aligned(16))) unsigned char lds_h[tile_h::kBytes];
     __shared__ __attribute__((aligned(16))) int lds_cols[32];
+    __shared__ fs_entries<V> entries;
     extern __shared__ __attribute__((aligned(16))) unsigned char dyn[];
     float *table = reinterpret_cast<float *>(dyn);
     uint8_t *lut = dyn + 4 * bias.n_buckets;
@@ -66,7 +69,7 @@ k_heads_rows(fs_walk a, fs_operand X, fs_operand Y, fs_operand H, fs_operand out
 
     BlockDesc d0 = block(0), d1 = block(1);
     int cols0 = fs_block_cols(a, d0, lane), cols1 = fs_block_cols(a, d1, lane);
-    uint32_t bits0 = fs_lane_bits<V>(a, it.x, 0, nblk, lane);
+    uint32_t bits0 = fs_row_bits<V>(a, it.x, 0, nblk, lane);
     // of the window: X's and g's rows, and lse (in units of log2) and D of row j
     fs_frag xf[KS], gf[KN], of[KN];
     float my_lse = 0.f;
@@ -84,9 +87,10 @@ k_heads_rows(fs_walk a, fs_operand X, fs_operand Y, fs_operand H, fs_operand out
     h.load(Hb, H.pitch, h_colb, cols0, lane);
     if (bias.n_buckets > 0) {
         fs_load_buckets(bias, lut, lane, 64);
-        for (int i = lane; i < bias.n_buckets; i += 64) table[i] = fs_widen<DT>(bias.table[head * bias.ld + i]) * 1.44269504088896340736f;
+        for (int i = lane; i < bias.n_buckets; i += 64) table[i] = fs_flagless_log2(fs_widen<DT>(bias.table[head * bias.ld + i]));
     }
     const fs_key key = fs_drop_key(drop, head);
+    const bool looks_up = bias.n_buckets > 0 || drop.state;
 
     fs_f4 acc[2 * KS];
     fs_clear(acc);
@@ -105,7 +109,7 @@ k_heads_rows(fs_walk a, fs_operand X, fs_operand Y, fs_operand H, fs_operand out
             y.load(Yb, Y.pitch, y_colb, cols1, lane);
             h.load(Hb, H.pitch, h_colb, cols1, lane);
             cols2 = fs_block_cols(a, d2, lane);
-            bits1 = fs_lane_bits<V>(a, it.x, step + 1, nblk, lane);
+            bits1 = fs_row_bits<V>(a, it.x, step + 1, nblk, lane);
         }
         const int row = d0.w * V + j;
         if (new_window) {
@@ -121,27 +125,48 @@ k_heads_rows(fs_walk a, fs_operand X, fs_operand Y, fs_operand H, fs_operand out
             if (d0.first && g == 0 && j < V && row < a.M) row_stats[(int64_t)head * a.M + row] = make_float2(lse2, D);
         }
         FS_WAVE_SYNC();
+        int n_entries = 0;
+        if (looks_up) {
+            n_entries = entries.make_list(bits0, lane);
+            entries.template look_up<false>(n_entries, lane, d0.w * V, cols0, lds_cols, bias, table, lut, drop, key);
+        }
         fs_f4 sc[2], gp[2];
 #pragma unroll
         for (int t = 0; t < 2; t++) {
             sc[t] = tile_y::template contract<DT>(lds_y, t, lane, xf);
             gp[t] = tile_h::template contract<DT>(lds_h, t, lane, gf);
         }
-        uint32_t kept = bits0;
-        if (drop.state) kept = fs_kept(bits0, key, drop.below, [&](int x) -> int2 { return make_int2(row, lds_cols[8 * g + x]); });
+        const uint32_t m8 = bits0 >> (8 * g);
         float ds[8];
+        if (looks_up) {
+            entries.values(ds, lane);
+#pragma unroll
+            for (int x = 0; x < 8; x++) {
+                const uint32_t kept = drop.state ? fs_bit_mask(__float_as_uint(ds[x]), 0) : ~0u;
+                gp[x >> 2][x & 3] = __uint_as_float(kept & __float_as_uint(gp[x >> 2][x & 3]));
+                ds[x] = fmaf(sc[x >> 2][x & 3], sl2, ds[x]);
+            }
+        } else {
+#pragma unroll
+            for (int x = 0; x < 8; x++) ds[x] = sc[x >> 2][x & 3] * sl2;
+        }
 #pragma unroll
         for (int x = 0; x < 8; x++) {
-            float t = sc[x >> 2][x & 3] * sl2;
-            int b = 0;
-            if (bias.n_buckets > 0) {
-                b = fs_bucket_of(lut, bias.reach, bias.shift, row, lds_cols[8 * g + x]);
-                t += table[b];
+            const float p = __builtin_amdgcn_exp2f(ds[x] - lse2);
+            ds[x] = fs_choose(fs_bit_mask(m8, x), p * fmaf(gp[x >> 2][x & 3], drop.factor, -D), 0.f);
+        }
+        if (bucket_sums) {
+            FS_WAVE_SYNC();
+            entries.put_values(ds, lane);
+            FS_WAVE_SYNC();
+            for (int r = lane; r < n_entries; r += 64) {
+                const int code = entries.list[r];
+                const float v = entries.value[(code >> 5 & 15) * entries.kPitch + (code & 31)];
+                float *cell = sums + COLS * (code >> 9) + (lane & (COLS - 1));
+#pragma unroll
+                for (int turn_ = 0; turn_ < 64 / COLS; turn_++)  // no two lanes of a turn share a cell
+                    if (lane / COLS == turn_) *cell += v;
             }
-            const float p = __builtin_amdgcn_exp2f(t - lse2);
-            const float gz = kept >> x & 1u ? gp[x >> 2][x & 3] * drop.factor : 0.f;
-            ds[x] = bits0 >> x & 1u ? p * (gz - D) : 0.f;
-            if (bucket_sums && (bits0 >> x & 1u)) fs_lds_add(sums + COLS * b + g * V + j, ds[x]);
         }
         const fs_frag sp = fs_round8<DT>(ds);
         if (d0.kb > 0) {
@@ -190,6 +215,7 @@ k_heads_cols(fs_walk a, int64_t rows, fs_operand X, fs_operand Y, fs_operand H, 
     __shared__ __attribute__((aligned(16))) unsigned char lds_g[tile_g::kBytes];
     __shared__ __attribute__((aligned(16))) int lds_rows[32];
     __shared__ __attribute__((aligned(16))) float2 lds_stats[32];
+    __shared__ fs_entries<V> entries;
     extern __shared__ __attribute__((aligned(16))) unsigned char dyn[];
     float *table = reinterpret_cast<float *>(dyn);  // of `share` heads
     uint8_t *lut = dyn + 4 * bias.n_buckets * share;
@@ -218,7 +244,7 @@ k_heads_cols(fs_walk a, int64_t rows, fs_operand X, fs_operand Y, fs_operand H, 
     };
     BlockDesc d0 = block(0), d1 = block(1);
     int rows0 = fs_block_cols(a, d0, lane), rows1 = fs_block_cols(a, d1, lane);
-    uint32_t bits0 = fs_lane_bits<V>(a, it.x, 0, nblk, lane), bits1 = fs_lane_bits<V>(a, it.x, 1, nblk, lane);
+    uint32_t bits0 = fs_row_bits<V>(a, it.x, 0, nblk, lane), bits1 = fs_row_bits<V>(a, it.x, 1, nblk, lane);
     fs_frag yf[KS], hf[KN];
     fs_load_window<V>(yf, Yb, Y.pitch, d, d0.w, a.M, lane);
     fs_load_window<V>(hf, Hb, H.pitch, N, d0.w, a.M, lane);
@@ -226,7 +252,7 @@ k_heads_cols(fs_walk a, int64_t rows, fs_operand X, fs_operand Y, fs_operand H, 
     if (bias.n_buckets > 0) {
         fs_load_buckets(bias, lut, lane, 64);
         for (int i = lane; i < bias.n_buckets * share; i += 64)
-            table[i] = fs_widen<DT>(bias.table[(kv * share + i / bias.n_buckets) * bias.ld + i % bias.n_buckets]) * 1.44269504088896340736f;
+            table[i] = fs_flagless_log2(fs_widen<DT>(bias.table[(kv * share + i / bias.n_buckets) * bias.ld + i % bias.n_buckets]));
     }
     fs_key keys = fs_key{0u, 0u};  // lane i: that of the group's head i
     if (drop.state) {
@@ -239,7 +265,8 @@ k_heads_cols(fs_walk a, int64_t rows, fs_operand X, fs_operand Y, fs_operand H, 
     fs_clear(acc_y);
     fs_clear(acc_h);
     bool from_first = d0.first;
-    int step = 0, member = 0;
+    const bool looks_up = bias.n_buckets > 0 || drop.state;
+    int step = 0, member = 0, n_entries = 0;
     for (;;) {  // a head of a block at a time
         const bool block_done = member + 1 == share, done = block_done && step + 1 == nblk;
         x_.put(lds_x, lane, d);
@@ -255,31 +282,44 @@ k_heads_cols(fs_walk a, int64_t rows, fs_operand X, fs_operand Y, fs_operand H, 
         if (block_done) {
             d2 = block(step + 2);
             rows2 = fs_block_cols(a, d2, lane);
-            bits2 = fs_lane_bits<V>(a, it.x, step + 2, nblk, lane);
+            bits2 = fs_row_bits<V>(a, it.x, step + 2, nblk, lane);
         }
         FS_WAVE_SYNC();
+        if (looks_up) {
+            const fs_key key = fs_key{(uint32_t)__builtin_amdgcn_readlane((int)keys.k0, member), (uint32_t)__builtin_amdgcn_readlane((int)keys.k1, member)};
+            if (member == 0) n_entries = entries.make_list(bits0, lane);
+            entries.template look_up<true>(n_entries, lane, d0.w * V, rows0, lds_rows, bias, table + member * bias.n_buckets, lut, drop, key);
+        }
         fs_f4 sc[2], gp[2];
 #pragma unroll
         for (int t = 0; t < 2; t++) {
             sc[t] = tile_x::template contract<DT>(lds_x, t, lane, yf);
             gp[t] = tile_g::template contract<DT>(lds_g, t, lane, hf);
         }
-        const int col = d0.w * V + j;
-        uint32_t kept = bits0;
-        if (drop.state) {
-            const fs_key key = fs_key{(uint32_t)__builtin_amdgcn_readlane((int)keys.k0, member), (uint32_t)__builtin_amdgcn_readlane((int)keys.k1, member)};
-            kept = fs_kept(bits0, key, drop.below, [&](int x) -> int2 { return make_int2(lds_rows[8 * g + x], col); });
-        }
+        const uint32_t m8 = bits0 >> (8 * g);
         float ds[8], w[8];
+        uint32_t kept[8];
+        if (looks_up) {
+            entries.values(ds, lane);
+#pragma unroll
+            for (int x = 0; x < 8; x++) {
+                kept[x] = fs_bit_mask(m8, x) & (drop.state ? fs_bit_mask(__float_as_uint(ds[x]), 0) : ~0u);
+                ds[x] = fmaf(sc[x >> 2][x & 3], sl2, ds[x]);
+            }
+        } else {
+#pragma unroll
+            for (int x = 0; x < 8; x++) {
+                kept[x] = fs_bit_mask(m8, x);
+                ds[x] = sc[x >> 2][x & 3] * sl2;
+            }
+        }
 #pragma unroll
         for (int x = 0; x < 8; x++) {
-            float t = sc[x >> 2][x & 3] * sl2;
-            if (bias.n_buckets > 0) t += table[member * bias.n_buckets + fs_bucket_of(lut, bias.reach, bias.shift, lds_rows[8 * g + x], col)];
             const float2 rs = lds_stats[8 * g + x];
-            const float p = __builtin_amdgcn_exp2f(t - rs.x);
-            const bool keep = kept >> x & 1u;
-            w[x] = keep ? p * kWeight : 0.f;
-            ds[x] = bits0 >> x & 1u ? p * ((keep ? gp[x >> 2][x & 3] * drop.factor : 0.f) - rs.y) : 0.f;
+            const float p = __builtin_amdgcn_exp2f(ds[x] - rs.x);
+            w[x] = __uint_as_float(kept[x] & __float_as_uint(p * kWeight));
+            const float gz = __uint_as_float(kept[x] & __float_as_uint(gp[x >> 2][x & 3]));
+            ds[x] = fs_choose(fs_bit_mask(m8, x), p * fmaf(gz, drop.factor, -rs.y), 0.f);
         }
         const fs_frag sy = fs_round8<DT>(ds), sh = fs_round8<DT>(w);
         if (d0.kb > 0) {
@@ -364,7 +404,7 @@ fs_status rows_launch(const fs_format *f, const call &c, const pieces &at)
 {
     const fs_launch_geometry geo = fs_launch_geometry_for(f, 1);
     float *tiles = c.work + at.tiles, *sums = c.n_grad > 0 ? c.work + at.sums : nullptr;
-    const size_t lds = (fs_bias_lds_bytes(c.bias.n_buckets, c.bias.reach) + 15) / 16 * 16 + (size_t)c.n_grad * 16 * V;
+    const size_t lds = (fs_bias_lds_bytes(c.bias.n_buckets, c.bias.reach) + 15) / 16 * 16 + (size_t)c.n_grad * 4 * kSumColumns;
     k_heads_rows<DT, V, KS, NT><<<dim3(geo.nbx, c.heads), 64, lds, c.st>>>(fs_walk_of(f, geo), c.X, c.Y, c.H, c.out, c.G, c.lse, c.heads / c.kv_heads, c.d, c.N,
                                                                           c.scale * 1.44269504088896340736f, c.scale, c.bias, c.drop, c.dX, (float2 *)c.work, tiles, sums);
     FS_LAUNCH_CHECK();
