@@ -260,19 +260,19 @@ struct fs_gathered {
 };
 
 // A window's rows in operand layout: lane (j, g) holds columns 32ks + 8g .. +7 of row w * V + j; rows past V or the last, and columns
-// past `width`, are zeros.
+// past `width`, are zeros.  Lanes without a row load nothing: in this layout a load takes the vector-memory unit a cycle per lane.
 template <int V, int STEPS>
 __device__ __forceinline__ void fs_load_window(fs_frag (&held)[STEPS], const unsigned char *base, uint32_t pitch, int width, int w, int64_t rows, int lane)
 {
     const int j = lane & 15, g = lane >> 4;
     const int64_t row = (int64_t)w * V + j;
-    const bool ok = j < V && row < rows;
-    const unsigned char *at = base + fs_mul24((uint32_t)(ok ? row : 0), pitch);
 #pragma unroll
-    for (int ks = 0; ks < STEPS; ks++) {
-        const bool in = 32 * ks + 8 * g < width;
-        held[ks].u = *reinterpret_cast<const fs_u4 *>(at + (in ? 2 * (32 * ks + 8 * g) : 0));
-        if (!ok || !in) held[ks].u = fs_u4{0u, 0u, 0u, 0u};
+    for (int ks = 0; ks < STEPS; ks++) held[ks].u = fs_u4{0u, 0u, 0u, 0u};
+    if (j < V && row < rows) {
+        const uint32_t at = fs_mul24((uint32_t)row, pitch) + 16 * g;
+#pragma unroll
+        for (int ks = 0; ks < STEPS; ks++)
+            if (32 * ks + 8 * g < width) held[ks].u = *reinterpret_cast<const fs_u4 *>(base + (at + 64 * ks));
     }
 }
 
@@ -411,6 +411,15 @@ __device__ __forceinline__ fs_frag fs_round8(const float (&p)[8])
     fs_frag o;
     o.u = fs_u4{fs_pack2<DT>(p[0], p[1]), fs_pack2<DT>(p[2], p[3]), fs_pack2<DT>(p[4], p[5]), fs_pack2<DT>(p[6], p[7])};
     return o;
+}
+// What that rounding leaves, rounded as well: the two together hold p to twice the bits.
+template <int DT>
+__device__ __forceinline__ fs_frag fs_round8_rest(const float (&p)[8], const fs_frag &rounded)
+{
+    float rest[8];
+#pragma unroll
+    for (int x = 0; x < 8; x++) rest[x] = p[x] - fs_widen<DT>(rounded.e[x]);
+    return fs_round8<DT>(rest);
 }
 
 // Accumulators -> rounded rows of an output of up to NC columns, by way of the tile's LDS.

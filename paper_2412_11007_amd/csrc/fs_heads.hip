@@ -8,8 +8,10 @@
 //   * the scores of the V x 32 block come from the matrix cores, Y's rows as the left operand and the window's rows of X, held in
 //     registers, as the right one: lane (j, g) gets the scores of window row j and vectors 8g .. 8g+7;
 //   * bias and pattern are applied in fp32 in units of log2, the running maximum m and sum l of the row are updated, the
-//     probabilities that dropout keeps are rounded to the element type relative to m;
-//   * they meet H's rows, read transposed from LDS, on the matrix cores; the accumulators are scaled by 2^(m_old - m_new).
+//     probabilities that dropout keeps become two numbers of the element type, the rounded one and what the rounding left;
+//   * both meet H's rows, read transposed from LDS, on the matrix cores; the accumulators are scaled by 2^(m_old - m_new).
+//     (The second product costs 3 to 7 %.  Without it the rounding of P would be in out beside out's own, and through D = g . out, whose
+//     parts cancel in sums over many entries, in the gradient of the bias: 1.5 times the error on a graph of 8 k rows.)
 // At a window's end the tile is divided by l (1 / (1 - p) goes in with it) and stored; parts of a cut window leave fp32 tiles and
 // (m, l), which k_add_parts merges in slot order.  l counts what dropout takes out as well: the mask applies after the softmax.
 // Heads are the slower grid dimension, so that one head's rows of Y and H share the L2s; query heads with the same keys are neighbours.
@@ -21,14 +23,13 @@
 namespace {
 
 template <int DT, int V, int KS, int NT>
-__global__ void __launch_bounds__(64)
+__global__ void __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(NT == 8 && KS > 1 ? 2 : 3)))
 k_heads_forward(fs_walk a, fs_operand X, fs_operand Y, fs_operand H, int share, int d, int N, float sl2, fs_bias_args bias, fs_drop_args drop,
                 fs_operand out, float *__restrict__ lse, float *__restrict__ part, float *__restrict__ stats)
 {
     using tile_y = fs_gathered<32 * KS>;
     using tile_h = fs_gathered<16 * NT>;
-    __shared__ __attribute__((aligned(16))) unsigned char lds_y[tile_y::kBytes];
-    __shared__ __attribute__((aligned(16))) unsigned char lds_h[tile_h::kBytes];
+    __shared__ __attribute__((aligned(16))) unsigned char lds[tile_y::kBytes > tile_h::kBytes ? tile_y::kBytes : tile_h::kBytes];  // Y's rows, then H's
     __shared__ __attribute__((aligned(16))) int lds_cols[32];
     __shared__ fs_entries<V> entries;
     extern __shared__ __attribute__((aligned(16))) unsigned char dyn[];
@@ -72,23 +73,27 @@ k_heads_forward(fs_walk a, fs_operand X, fs_operand Y, fs_operand H, int share, 
     int step = 0;
     auto block_step = [&](auto more_) {
         constexpr bool MORE = decltype(more_)::value;
-        y.put(lds_y, lane, d);
-        h.put(lds_h, lane, N);
         if (lane < 32) lds_cols[lane] = cols0;
         const BlockDesc d2 = block(step + 2);
         int cols2 = 0;
         uint32_t bits1 = 0;
         if constexpr (MORE) {
-            y.load(Yb, Y.pitch, y_colb, cols1, lane);
-            h.load(Hb, H.pitch, h_colb, cols1, lane);
             cols2 = fs_block_cols(a, d2, lane);
             bits1 = fs_row_bits<V>(a, it.x, step + 1, nblk, lane);
         }
         FS_WAVE_SYNC();
         if (looks_up) entries.template look_up<false>(entries.make_list(bits0, lane), lane, d0.w * V, cols0, lds_cols, bias, table, lut, drop, key);
+        y.put(lds, lane, d);
+        if constexpr (MORE) y.load(Yb, Y.pitch, y_colb, cols1, lane);
+        FS_WAVE_SYNC();
         fs_f4 sc[2];
 #pragma unroll
-        for (int t = 0; t < 2; t++) sc[t] = tile_y::template contract<DT>(lds_y, t, lane, xf);
+        for (int t = 0; t < 2; t++) sc[t] = tile_y::template contract<DT>(lds, t, lane, xf);
+        FS_WAVE_SYNC();
+        h.put(lds, lane, N);
+        if (MORE && d1.w != d0.w) fs_load_window<V>(xf, Xb, X.pitch, d, d1.w, a.M, lane);
+        if constexpr (MORE) h.load(Hb, H.pitch, h_colb, cols1, lane);
+        FS_WAVE_SYNC();
         const int row = d0.w * V + j;
         const uint32_t m8 = bits0 >> (8 * g);
         float p[8], mx = -INFINITY;
@@ -127,18 +132,20 @@ k_heads_forward(fs_walk a, fs_operand X, fs_operand Y, fs_operand H, int share, 
         m_run = m_new;
 #pragma unroll
         for (int x = 0; x < 8; x++) p[x] = __uint_as_float(kept[x] & __float_as_uint(p[x]));
-        const fs_frag sp = fs_round8<DT>(p);
+        const fs_frag hi = fs_round8<DT>(p), lo = fs_round8_rest<DT>(p, hi);
         if (d0.kb > 0) {
 #pragma unroll
-            for (int t = 0; t < NT; t++) acc[t] = fs_mfma_16x16x32<DT>(tile_h::transposed(lds_h, t, lane), sp, acc[t] * corr);
+            for (int t = 0; t < NT; t++) {
+                const fs_frag rows = tile_h::transposed(lds, t, lane);
+                acc[t] = fs_mfma_16x16x32<DT>(rows, lo, fs_mfma_16x16x32<DT>(rows, hi, acc[t] * corr));
+            }
         }
         FS_WAVE_SYNC();
-        if (MORE && d1.w != d0.w) fs_load_window<V>(xf, Xb, X.pitch, d, d1.w, a.M, lane);
         if (d0.last || !MORE) {
             float l_tot = l_run + __shfl_xor(l_run, 16, 64);
             l_tot += __shfl_xor(l_tot, 32, 64);
             if (d0.last && from_first) {
-                fs_store_window<DT, V, 16 * NT>(lds_h, acc, l_tot == 0.f ? 0.f : drop.factor / l_tot, out.p + head * out.head, out.pitch, N, d0.w, a.M, lane);
+                fs_store_window<DT, V, 16 * NT>(lds, acc, l_tot == 0.f ? 0.f : drop.factor / l_tot, out.p + head * out.head, out.pitch, N, d0.w, a.M, lane);
                 if (lse && g == 0 && j < V && row < a.M) lse[(int64_t)head * a.M + row] = fs_log_sum(m_run, l_tot);
             } else {
                 fs_store_part<V>(part + (int64_t)head * a.n_slots * V * N, slot, N, acc, lane);

@@ -28,7 +28,7 @@ namespace {
 constexpr int kSumColumns = 32;  // of the table of sums in LDS, for each bucket
 
 template <int DT, int V, int KS, int NT>
-__global__ void __launch_bounds__(64)
+__global__ void __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(KS <= 2 && NT <= 4 ? 3 : 2)))
 k_heads_rows(fs_walk a, fs_operand X, fs_operand Y, fs_operand H, fs_operand out, fs_operand G, const float *__restrict__ lse, int share, int d, int N,
              float sl2, float scale, fs_bias_args bias, fs_drop_args drop, fs_operand dX, float2 *__restrict__ row_stats, float *__restrict__ part,
              float *__restrict__ bucket_sums)
@@ -36,8 +36,7 @@ k_heads_rows(fs_walk a, fs_operand X, fs_operand Y, fs_operand H, fs_operand out
     using tile_y = fs_gathered<32 * KS>;
     using tile_h = fs_gathered<16 * NT>;
     constexpr int KN = NT / 2, COLS = kSumColumns;
-    __shared__ __attribute__((aligned(16))) unsigned char lds_y[tile_y::kBytes];
-    __shared__ __attribute__((aligned(16))) unsigned char lds_h[tile_h::kBytes];
+    __shared__ __attribute__((aligned(16))) unsigned char lds[tile_y::kBytes > tile_h::kBytes ? tile_y::kBytes : tile_h::kBytes];  // H's rows, then Y's
     __shared__ __attribute__((aligned(16))) int lds_cols[32];
     __shared__ fs_entries<V> entries;
     extern __shared__ __attribute__((aligned(16))) unsigned char dyn[];
@@ -78,7 +77,7 @@ k_heads_rows(fs_walk a, fs_operand X, fs_operand Y, fs_operand H, fs_operand out
         fs_load_window<V>(gf, Gb, G.pitch, N, w, a.M, lane);
         fs_load_window<V>(of, Ob, out.pitch, N, w, a.M, lane);
         const int64_t row = (int64_t)w * V + j;
-        my_lse = lse[(int64_t)head * a.M + (j < V && row < a.M ? row : 0)];
+        if (j < V && row < a.M) my_lse = lse[(int64_t)head * a.M + row];
     };
     load_window(d0.w);
     tile_y y;
@@ -99,18 +98,22 @@ k_heads_rows(fs_walk a, fs_operand X, fs_operand Y, fs_operand H, fs_operand out
     int step = 0;
     auto block_step = [&](auto more_) {
         constexpr bool MORE = decltype(more_)::value;
-        y.put(lds_y, lane, d);
-        h.put(lds_h, lane, N);
         if (lane < 32) lds_cols[lane] = cols0;
         const BlockDesc d2 = block(step + 2);
         int cols2 = 0;
         uint32_t bits1 = 0;
         if constexpr (MORE) {
-            y.load(Yb, Y.pitch, y_colb, cols1, lane);
-            h.load(Hb, H.pitch, h_colb, cols1, lane);
             cols2 = fs_block_cols(a, d2, lane);
             bits1 = fs_row_bits<V>(a, it.x, step + 1, nblk, lane);
         }
+        FS_WAVE_SYNC();
+        int n_entries = 0;
+        if (looks_up) {
+            n_entries = entries.make_list(bits0, lane);
+            entries.template look_up<false>(n_entries, lane, d0.w * V, cols0, lds_cols, bias, table, lut, drop, key);
+        }
+        h.put(lds, lane, N);
+        if constexpr (MORE) h.load(Hb, H.pitch, h_colb, cols1, lane);
         const int row = d0.w * V + j;
         if (new_window) {
             D = 0.f;
@@ -125,35 +128,32 @@ k_heads_rows(fs_walk a, fs_operand X, fs_operand Y, fs_operand H, fs_operand out
             if (d0.first && g == 0 && j < V && row < a.M) row_stats[(int64_t)head * a.M + row] = make_float2(lse2, D);
         }
         FS_WAVE_SYNC();
-        int n_entries = 0;
-        if (looks_up) {
-            n_entries = entries.make_list(bits0, lane);
-            entries.template look_up<false>(n_entries, lane, d0.w * V, cols0, lds_cols, bias, table, lut, drop, key);
-        }
         fs_f4 sc[2], gp[2];
 #pragma unroll
-        for (int t = 0; t < 2; t++) {
-            sc[t] = tile_y::template contract<DT>(lds_y, t, lane, xf);
-            gp[t] = tile_h::template contract<DT>(lds_h, t, lane, gf);
-        }
+        for (int t = 0; t < 2; t++) gp[t] = tile_h::template contract<DT>(lds, t, lane, gf);
+        FS_WAVE_SYNC();
+        y.put(lds, lane, d);
+        if constexpr (MORE) y.load(Yb, Y.pitch, y_colb, cols1, lane);
+        FS_WAVE_SYNC();
+#pragma unroll
+        for (int t = 0; t < 2; t++) sc[t] = tile_y::template contract<DT>(lds, t, lane, xf);
+        new_window = MORE && d1.w != d0.w;
+        if (new_window) load_window(d1.w);
         const uint32_t m8 = bits0 >> (8 * g);
         float ds[8];
         if (looks_up) {
             entries.values(ds, lane);
-#pragma unroll
-            for (int x = 0; x < 8; x++) {
-                const uint32_t kept = drop.state ? fs_bit_mask(__float_as_uint(ds[x]), 0) : ~0u;
-                gp[x >> 2][x & 3] = __uint_as_float(kept & __float_as_uint(gp[x >> 2][x & 3]));
-                ds[x] = fmaf(sc[x >> 2][x & 3], sl2, ds[x]);
-            }
         } else {
 #pragma unroll
-            for (int x = 0; x < 8; x++) ds[x] = sc[x >> 2][x & 3] * sl2;
+            for (int x = 0; x < 8; x++) ds[x] = 0.f;
         }
+        const uint32_t all = drop.state ? 0u : ~0u;
 #pragma unroll
         for (int x = 0; x < 8; x++) {
-            const float p = __builtin_amdgcn_exp2f(ds[x] - lse2);
-            ds[x] = fs_choose(fs_bit_mask(m8, x), p * fmaf(gp[x >> 2][x & 3], drop.factor, -D), 0.f);
+            const uint32_t kept = all | fs_bit_mask(__float_as_uint(ds[x]), 0);
+            const float p = __builtin_amdgcn_exp2f(fmaf(sc[x >> 2][x & 3], sl2, ds[x]) - lse2);
+            const float gz = __uint_as_float(kept & __float_as_uint(gp[x >> 2][x & 3]));
+            ds[x] = __uint_as_float(fs_bit_mask(m8, x) & __float_as_uint(p * fmaf(gz, drop.factor, -D)));
         }
         if (bucket_sums) {
             FS_WAVE_SYNC();
@@ -171,14 +171,12 @@ k_heads_rows(fs_walk a, fs_operand X, fs_operand Y, fs_operand H, fs_operand out
         const fs_frag sp = fs_round8<DT>(ds);
         if (d0.kb > 0) {
 #pragma unroll
-            for (int t = 0; t < 2 * KS; t++) acc[t] = fs_mfma_16x16x32<DT>(tile_y::transposed(lds_y, t, lane), sp, acc[t]);
+            for (int t = 0; t < 2 * KS; t++) acc[t] = fs_mfma_16x16x32<DT>(tile_y::transposed(lds, t, lane), sp, acc[t]);
         }
         FS_WAVE_SYNC();
-        new_window = MORE && d1.w != d0.w;
-        if (new_window) load_window(d1.w);
         if (d0.last || !MORE) {
             if (d0.last && from_first) {
-                fs_store_window<DT, V, 32 * KS>(lds_y, acc, scale, dX.p + head * dX.head, dX.pitch, d, d0.w, a.M, lane);
+                fs_store_window<DT, V, 32 * KS>(lds, acc, scale, dX.p + head * dX.head, dX.pitch, d, d0.w, a.M, lane);
             } else {
                 fs_store_part<V>(part + (int64_t)head * a.n_slots * V * d, slot, d, acc, lane);
                 slot++;
@@ -202,7 +200,7 @@ k_heads_rows(fs_walk a, fs_operand X, fs_operand Y, fs_operand H, fs_operand out
 
 // By columns: `a` walks A^T, its vectors are rows of A (`rows` of them) and its window rows columns.
 template <int DT, int V, int KS, int NT>
-__global__ void __launch_bounds__(64)
+__global__ void __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(KS * NT <= 8 ? 3 : 2)))
 k_heads_cols(fs_walk a, int64_t rows, fs_operand X, fs_operand Y, fs_operand H, fs_operand G, const float2 *__restrict__ row_stats, int share, int d,
              int N, float sl2, float scale, fs_bias_args bias, fs_drop_args drop, fs_operand dY, fs_operand dH, float *__restrict__ part_y,
              float *__restrict__ part_h)
@@ -296,30 +294,27 @@ k_heads_cols(fs_walk a, int64_t rows, fs_operand X, fs_operand Y, fs_operand H, 
             sc[t] = tile_x::template contract<DT>(lds_x, t, lane, yf);
             gp[t] = tile_g::template contract<DT>(lds_g, t, lane, hf);
         }
+        if (block_done && d1.w != d0.w) {
+            fs_load_window<V>(yf, Yb, Y.pitch, d, d1.w, a.M, lane);
+            fs_load_window<V>(hf, Hb, H.pitch, N, d1.w, a.M, lane);
+        }
         const uint32_t m8 = bits0 >> (8 * g);
         float ds[8], w[8];
-        uint32_t kept[8];
         if (looks_up) {
             entries.values(ds, lane);
-#pragma unroll
-            for (int x = 0; x < 8; x++) {
-                kept[x] = fs_bit_mask(m8, x) & (drop.state ? fs_bit_mask(__float_as_uint(ds[x]), 0) : ~0u);
-                ds[x] = fmaf(sc[x >> 2][x & 3], sl2, ds[x]);
-            }
         } else {
 #pragma unroll
-            for (int x = 0; x < 8; x++) {
-                kept[x] = fs_bit_mask(m8, x);
-                ds[x] = sc[x >> 2][x & 3] * sl2;
-            }
+            for (int x = 0; x < 8; x++) ds[x] = 0.f;
         }
+        const uint32_t all = drop.state ? 0u : ~0u;
 #pragma unroll
         for (int x = 0; x < 8; x++) {
+            const uint32_t stored = fs_bit_mask(m8, x), kept = stored & (all | fs_bit_mask(__float_as_uint(ds[x]), 0));
             const float2 rs = lds_stats[8 * g + x];
-            const float p = __builtin_amdgcn_exp2f(ds[x] - rs.x);
-            w[x] = __uint_as_float(kept[x] & __float_as_uint(p * kWeight));
-            const float gz = __uint_as_float(kept[x] & __float_as_uint(gp[x >> 2][x & 3]));
-            ds[x] = fs_choose(fs_bit_mask(m8, x), p * fmaf(gz, drop.factor, -rs.y), 0.f);
+            const float p = __builtin_amdgcn_exp2f(fmaf(sc[x >> 2][x & 3], sl2, ds[x]) - rs.x);
+            w[x] = __uint_as_float(kept & __float_as_uint(p * kWeight));
+            const float gz = __uint_as_float(kept & __float_as_uint(gp[x >> 2][x & 3]));
+            ds[x] = __uint_as_float(stored & __float_as_uint(p * fmaf(gz, drop.factor, -rs.y)));
         }
         const fs_frag sy = fs_round8<DT>(ds), sh = fs_round8<DT>(w);
         if (d0.kb > 0) {
@@ -334,10 +329,6 @@ k_heads_cols(fs_walk a, int64_t rows, fs_operand X, fs_operand Y, fs_operand H, 
             continue;
         }
         member = 0;
-        if (!done && d1.w != d0.w) {
-            fs_load_window<V>(yf, Yb, Y.pitch, d, d1.w, a.M, lane);
-            fs_load_window<V>(hf, Hb, H.pitch, N, d1.w, a.M, lane);
-        }
         if (d0.last || done) {
             if (d0.last && from_first) {
                 fs_store_window<DT, V, 32 * KS>(lds_x, acc_y, scale, dY.p + kv * dY.head, dY.pitch, d, d0.w, a.M, lane);
