@@ -34,11 +34,21 @@ k_edges(const int4 *__restrict__ blk_desc, int n_blocks, const uint32_t *__restr
     constexpr int LANES = 4 * V;   // lanes of a block
     __shared__ __attribute__((aligned(16))) int cols_all[WAVES][PER][32];
     __shared__ uint32_t bits_all[WAVES][16];
+    __shared__ int2 blocks_all[WAVES][PER];  // OP_DROPOUT: {first row, kb's reciprocal | kb}
+    __shared__ __attribute__((aligned(16))) uint16_t list_all[OP == OP_DROPOUT ? WAVES : 1][512];  // OP_DROPOUT: the stored elements of a round
+    __shared__ __attribute__((aligned(16))) uint8_t kept_all[OP == OP_DROPOUT ? WAVES : 1][512];   // and which are kept, by place
     extern __shared__ __attribute__((aligned(16))) unsigned char dyn[];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, head = blockIdx.y;
     float *table = reinterpret_cast<float *>(dyn);                   // OP_BIAS: of the head
     uint8_t *lut = dyn + (OP == OP_BIAS ? bias.n_buckets * 4 : 0);
     float *mine = reinterpret_cast<float *>(dyn + (2 * bias.reach + 1 + 15) / 16 * 16) + lane;  // OP_GRADIENT: + 64 * bucket
+    in += head * n_el;
+    if constexpr (OP != OP_GRADIENT) out += head * n_el;
+    int *cols = cols_all[wave][lane / LANES];
+    int2 *block_of = blocks_all[wave];
+    uint32_t *bits = bits_all[wave] + (lane / LANES) * V;
+    const int e0 = 8 * (lane % LANES);  // of the block
+
     fs_key key = fs_key{0u, 0u};
     if constexpr (OP == OP_DROPOUT) {
         key = fs_drop_key(drop, head);
@@ -47,21 +57,18 @@ k_edges(const int4 *__restrict__ blk_desc, int n_blocks, const uint32_t *__restr
         if constexpr (OP == OP_BIAS) {
             for (int i = threadIdx.x; i < bias.n_buckets; i += WAVES * 64) table[i] = fs_widen<DT>(bias.table[head * bias.ld + i]);
         } else {
-            for (int i = 0; i < bias.n_buckets; i++) mine[64 * i] = 0.f;
+            for (int i = lane; i < bias.n_buckets * 16; i += 64) reinterpret_cast<fs_f4 *>(mine - lane)[i] = fs_f4{0.f, 0.f, 0.f, 0.f};
         }
         __syncthreads();
     }
-    in += head * n_el;
-    if constexpr (OP != OP_GRADIENT) out += head * n_el;
-    int *cols = cols_all[wave][lane / LANES];
-    uint32_t *bits = bits_all[wave] + (lane / LANES) * V;
-    const int e0 = 8 * (lane % LANES);  // of the block
-
     const int step = gridDim.x * WAVES * PER;
-    for (int x0 = (blockIdx.x * WAVES + wave) * PER; x0 < n_blocks; x0 += step) {
+    int x0 = (blockIdx.x * WAVES + wave) * PER;
+    int4 ahead = blk_desc[min(x0 + lane / LANES, n_blocks - 1)];  // descriptors are read a round ahead (values too: slower, a third fewer wavefronts fit)
+    for (; x0 < n_blocks; x0 += step) {
         const int x = x0 + lane / LANES;
-        const int4 desc = blk_desc[min(x, n_blocks - 1)];
-        const int kb = x < n_blocks ? desc.y & 255 : 0;
+        const int4 desc = ahead;
+        ahead = blk_desc[min(x + step, n_blocks - 1)];
+        const int kb = x < n_blocks ? desc.y & 255 : 0, row0 = desc.z * V;
         const int64_t first = (int64_t)V * desc.x;
         const int own = min(8, V * kb - e0);  // elements of the lane: eight, four (V = 4, odd width) or none
         fs_frag v;
@@ -84,29 +91,66 @@ k_edges(const int4 *__restrict__ blk_desc, int n_blocks, const uint32_t *__restr
                 if (k < own) m8 |= (bits[r] >> (e0 + k - r * kb) & 1u) << k;
             }
         }
-        const int row0 = desc.z * V;
         if constexpr (OP == OP_DROPOUT) {
-            const uint32_t kept = fs_kept(m8, key, drop.below, [&](int k) -> int2 {
-                const int r = row_of(k);
-                return make_int2(row0 + r, cols[e0 + k - r * kb]);
-            });
+            // the stored elements are dealt out to the lanes: an eighth of the places in a power-law graph (R-MAT of 65 k rows: lane by
+            // lane, four words in a row, 17 us; lognormal graph, two heads, 124)
+            uint16_t *list = list_all[wave];
+            uint8_t *is_kept = kept_all[wave];
+            const int own_n = __popc(m8);
+            int sum = own_n;
+            sum += __builtin_amdgcn_update_dpp(0, sum, 0x111, 0xF, 0xF, true);  // row_shr:1, 2, 4, 8
+            sum += __builtin_amdgcn_update_dpp(0, sum, 0x112, 0xF, 0xF, true);
+            sum += __builtin_amdgcn_update_dpp(0, sum, 0x114, 0xF, 0xF, true);
+            sum += __builtin_amdgcn_update_dpp(0, sum, 0x118, 0xF, 0xF, true);
+            sum += __builtin_amdgcn_update_dpp(0, sum, 0x142, 0xA, 0xF, true);  // row_bcast:15, 31
+            sum += __builtin_amdgcn_update_dpp(0, sum, 0x143, 0xC, 0xF, true);
+            int at = sum - own_n;
+            for (uint32_t m = m8; m; m &= m - 1) list[at++] = (uint16_t)(8 * lane + __builtin_ctz(m));
+            const int n = __builtin_amdgcn_readlane(sum, 63);
+            if (lane % LANES == 0) block_of[lane / LANES] = make_int2(row0, (int)inv << 8 | kb);
+            FS_WAVE_SYNC();
+            for (int i = lane; i < n; i += 64) {
+                const int place = list[i], b = place / (8 * LANES), e = place % (8 * LANES);
+                const int2 of = block_of[b];
+                const int r = (uint32_t)e * ((uint32_t)of.y >> 8) >> 16, c = e - r * (of.y & 255);
+                is_kept[place] = fs_threefry<13>(key, (uint32_t)(of.x + r), (uint32_t)cols_all[wave][b][c]).k0 >= drop.below;
+            }
+            FS_WAVE_SYNC();
+            const uint2 mine8 = *reinterpret_cast<const uint2 *>(is_kept + 8 * lane);
+            uint32_t kept = 0;
+#pragma unroll
+            for (int k = 0; k < 8; k++) kept |= ((k < 4 ? mine8.x : mine8.y) >> (8 * (k & 3)) & 1u) << k;
+            kept &= m8;
             float y[8];
 #pragma unroll
             for (int k = 0; k < 8; k++) y[k] = kept >> k & 1u ? fs_widen<DT>(v.e[k]) * drop.factor : 0.f;
             v.u = fs_u4{fs_pack2<DT>(y[0], y[1]), fs_pack2<DT>(y[2], y[3]), fs_pack2<DT>(y[4], y[5]), fs_pack2<DT>(y[6], y[7])};
         } else {
-            float y[8];
+            int bucket[8];  // of all eight places at once: their reads do not wait for one another
+            if (kb == 32) {
+                const int4 lo = *reinterpret_cast<const int4 *>(cols + (e0 & 31)), hi = *reinterpret_cast<const int4 *>(cols + (e0 & 31) + 4);
+                const int col[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
 #pragma unroll
-            for (int k = 0; k < 8; k++) {
-                y[k] = 0.f;
-                if (m8 >> k & 1u) {
+                for (int k = 0; k < 8; k++) bucket[k] = fs_bucket_of(lut, bias.reach, bias.shift, row0 + (e0 >> 5), col[k]);
+            } else {
+#pragma unroll
+                for (int k = 0; k < 8; k++) {
                     const int r = row_of(k);
-                    const int b = fs_bucket_of(lut, bias.reach, bias.shift, row0 + r, cols[e0 + k - r * kb]);
-                    if constexpr (OP == OP_BIAS) y[k] = fmaf(scale, fs_widen<DT>(v.e[k]), table[b]);
-                    else mine[64 * b] += fs_widen<DT>(v.e[k]);
+                    bucket[k] = fs_bucket_of(lut, bias.reach, bias.shift, row0 + r, cols[(e0 + k - r * kb) & 31]);
                 }
             }
-            if constexpr (OP == OP_BIAS) v.u = fs_u4{fs_pack2<DT>(y[0], y[1]), fs_pack2<DT>(y[2], y[3]), fs_pack2<DT>(y[4], y[5]), fs_pack2<DT>(y[6], y[7])};
+            if constexpr (OP == OP_BIAS) {
+                float y[8];
+#pragma unroll
+                for (int k = 0; k < 8; k++) y[k] = table[bucket[k]];
+#pragma unroll
+                for (int k = 0; k < 8; k++) y[k] = m8 >> k & 1u ? fmaf(scale, fs_widen<DT>(v.e[k]), y[k]) : 0.f;
+                v.u = fs_u4{fs_pack2<DT>(y[0], y[1]), fs_pack2<DT>(y[2], y[3]), fs_pack2<DT>(y[4], y[5]), fs_pack2<DT>(y[6], y[7])};
+            } else {
+#pragma unroll
+                for (int k = 0; k < 8; k++)
+                    if (m8 >> k & 1u) mine[64 * bucket[k]] += fs_widen<DT>(v.e[k]);
+            }
         }
         if constexpr (OP != OP_GRADIENT) {
             if (own == 8) *reinterpret_cast<fs_u4_unaligned *>(out + first + e0) = v.u;
@@ -121,13 +165,13 @@ k_edges(const int4 *__restrict__ blk_desc, int n_blocks, const uint32_t *__restr
     }
 }
 
-// Adds n tables of n_buckets sums, a contiguous share of them per workgroup: thread (r, b) those r, r + R, ... of its share, R = 256
+// Adds n tables of n_buckets sums, a contiguous share of them per workgroup: thread (r, b) those r, r + R, ... of its share, R = 1024
 // over the buckets' power of two; then the R sums of a bucket in order.  DT < 0: to fp32 tables, one a workgroup.
 template <int DT>
-__global__ void __launch_bounds__(256) k_bucket_sums(const float *__restrict__ sums, int n, int n_buckets, int log2_buckets, void *__restrict__ to)
+__global__ void __launch_bounds__(1024) k_bucket_sums(const float *__restrict__ sums, int n, int n_buckets, int log2_buckets, void *__restrict__ to)
 {
-    __shared__ float part[256];
-    const int b = threadIdx.x & ((1 << log2_buckets) - 1), r = threadIdx.x >> log2_buckets, R = 256 >> log2_buckets;
+    __shared__ float part[1024];
+    const int b = threadIdx.x & ((1 << log2_buckets) - 1), r = threadIdx.x >> log2_buckets, R = 1024 >> log2_buckets;
     const int head = blockIdx.y, share = (n + gridDim.x - 1) / gridDim.x, i0 = blockIdx.x * share, i1 = min(n, i0 + share);
     const float *from = sums + (int64_t)head * n * n_buckets + min(b, n_buckets - 1);
     float t = 0.f;
@@ -191,15 +235,15 @@ fs_status fs_bucket_sums_launch(int dtype, int heads, int n, int n_buckets, floa
 {
     int log2_buckets = 0;
     while (1 << log2_buckets < n_buckets) log2_buckets++;
-    if (n > 4 * kBucketSumGroups) {
+    if (n > 1024) {
         float *part = sums + (size_t)heads * n * n_buckets;
-        k_bucket_sums<-1><<<dim3(kBucketSumGroups, heads), 256, 0, st>>>(sums, n, n_buckets, log2_buckets, part);
+        k_bucket_sums<-1><<<dim3(kBucketSumGroups, heads), 1024, 0, st>>>(sums, n, n_buckets, log2_buckets, part);
         FS_LAUNCH_CHECK();
         sums = part;
         n = kBucketSumGroups;
     }
-    if (dtype == FS_BF16) k_bucket_sums<FS_BF16><<<dim3(1, heads), 256, 0, st>>>(sums, n, n_buckets, log2_buckets, grad);
-    else k_bucket_sums<FS_F16><<<dim3(1, heads), 256, 0, st>>>(sums, n, n_buckets, log2_buckets, grad);
+    if (dtype == FS_BF16) k_bucket_sums<FS_BF16><<<dim3(1, heads), 1024, 0, st>>>(sums, n, n_buckets, log2_buckets, grad);
+    else k_bucket_sums<FS_F16><<<dim3(1, heads), 1024, 0, st>>>(sums, n, n_buckets, log2_buckets, grad);
     FS_LAUNCH_CHECK();
     return FS_OK;
 }

@@ -103,22 +103,6 @@ __device__ __forceinline__ int fs_bucket_of(const uint8_t *lut, int reach, int s
     return lut[min(max(r, -reach), reach) + reach];
 }
 
-// Which of a lane's eight positions (m8: those that are stored) are kept.  at(x): the counter of position x.
-template <typename Counter>
-__device__ __forceinline__ uint32_t fs_kept(uint32_t m8, fs_key key, uint32_t below, Counter at)
-{
-    uint32_t kept = 0;
-    for (uint32_t m = m8; m; m &= m - 1) {
-        const int x = __builtin_ctz(m);
-        const int2 c = at(x);  // row, column of A
-        if (fs_threefry<13>(key, (uint32_t)c.x, (uint32_t)c.y).k0 >= below) kept |= 1u << x;
-    }
-    return kept;
-}
-
-// Adds to a lane's own cell of a table in LDS (one instruction, nothing to wait for).
-__device__ __forceinline__ void fs_lds_add(float *cell, float v) { unsafeAtomicAdd(cell, v); }
-
 // A wavefront's table of COLS sums per bucket (a power of two) -> one sum per bucket.  The order of the columns differs from
 // bucket to bucket, so that the lanes read different banks, and is always the same.
 template <int COLS>
