@@ -428,73 +428,6 @@ __device__ __forceinline__ void fs_store_part(float *tiles, int slot, int width,
     fs_store_partial_tile<V, NT>(tiles, slot, width, (uint32_t)((g * V + j) * 16), acc, j < V, NT * 16 <= width, 0, g);
 }
 
-// Adds the partial tiles of one cut window and 32 columns, in slot order, one wavefront each, for every head.  SM: the parts carry
-// (maximum m, sum l) per row of a softmax in units of log2, and with m* the largest m of a row
-//   out = factor * sum_k 2^(m_k - m*) tile_k / sum_k 2^(m_k - m*) l_k,   lse = ln 2 * (m* + log2 of that sum).
-// Lane (row r = lane % V, q = lane / V) first walks the parts q, q + 64/V, ...; tiles are read in their storage order, sixteen loads in
-// flight, and the rounded rows leave through LDS.
-template <int DT, int V, bool SM>
-__global__ void __launch_bounds__(64)
-k_add_parts(const int4 *__restrict__ split_windows, const float *__restrict__ part, const float *__restrict__ stats, int n_slots, int N,
-            fs_operand out, float factor, int64_t M, float *__restrict__ lse)
-{
-    constexpr int CH = 32, KQ = 64 / V;
-    __shared__ __attribute__((aligned(16))) uint16_t out_t[V][CH + 8];
-    const int n_chunks = (N + CH - 1) / CH, head = blockIdx.y;
-    const int4 sw = split_windows[blockIdx.x / n_chunks];
-    const int w = sw.x, p0 = sw.y, cnt = sw.z;
-    const int lane = threadIdx.x, r = lane % V, q = lane / V;
-    const int c0 = (blockIdx.x % n_chunks) * CH, nc = min(CH, N - c0);
-    const float *st = SM ? stats + ((int64_t)head * n_slots + p0) * 2 * V : nullptr;
-    float use = 0.f, inv = factor;
-    if constexpr (SM) {
-        float top = -INFINITY;
-        for (int k = q; k < cnt; k += KQ) top = fmaxf(top, st[(int64_t)k * 2 * V + r]);
-#pragma unroll
-        for (int o = V; o < 64; o <<= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
-        use = top == -INFINITY ? 0.f : top;
-        float total = 0.f;
-        for (int k = q; k < cnt; k += KQ) total += st[(int64_t)k * 2 * V + V + r] * __builtin_amdgcn_exp2f(st[(int64_t)k * 2 * V + r] - use);
-#pragma unroll
-        for (int o = V; o < 64; o <<= 1) total += __shfl_xor(total, o, 64);
-        inv = total == 0.f ? 0.f : factor / total;
-        if (lse && c0 == 0 && q == 0 && (int64_t)w * V + r < M) lse[(int64_t)head * M + (int64_t)w * V + r] = fs_log_sum(use, total);
-    }
-    const int64_t tile4 = (int64_t)V * N / 4;
-    const fs_f4 *src0 = reinterpret_cast<const fs_f4 *>(part) + ((int64_t)head * n_slots + p0) * tile4 + (c0 / 4) * V;
-    for (int idx = lane; idx < (nc / 4) * V; idx += 64) {  // idx % V == r
-        const int ct = idx / (4 * V), rem = idx - ct * 4 * V, g = rem / V, j = rem - g * V;
-        const fs_f4 *src = src0 + idx;
-        fs_f4 sum = fs_f4{0.f, 0.f, 0.f, 0.f};
-        for (int k = 0; k < cnt; k += 16) {
-            fs_f4 v[16];
-            float wk[16];
-#pragma unroll
-            for (int u = 0; u < 16; u++) {
-                const int kk = min(k + u, cnt - 1);
-                v[u] = src[(int64_t)kk * tile4];
-                wk[u] = SM ? st[(int64_t)kk * 2 * V + j] : 0.f;
-            }
-#pragma unroll
-            for (int u = 0; u < 16; u++)
-                if (k + u < cnt) sum += SM ? v[u] * __builtin_amdgcn_exp2f(wk[u] - use) : v[u];
-        }
-        uint2 o;
-        o.x = fs_pack2<DT>(sum[0] * inv, sum[1] * inv);
-        o.y = fs_pack2<DT>(sum[2] * inv, sum[3] * inv);
-        *reinterpret_cast<uint2 *>(&out_t[j][16 * ct + 4 * g]) = o;
-    }
-    __syncthreads();
-    const int c8n = nc / 8;
-    for (int t = lane; t < V * c8n; t += 64) {
-        const int j = t / c8n, c8 = t - j * c8n;
-        const int64_t row = (int64_t)w * V + j;
-        if (row < M)
-            __builtin_nontemporal_store(*reinterpret_cast<const fs_u4 *>(&out_t[j][8 * c8]),
-                                        reinterpret_cast<fs_u4 *>(out.p + head * out.head + row * out.pitch + 2 * (c0 + 8 * c8)));
-    }
-}
-
 // Floats of the partial tiles of one kernel.
 inline size_t fs_part_floats(const fs_format *f, int64_t heads, int64_t columns) { return (size_t)heads * (size_t)f->n_split_items * (size_t)f->V * (size_t)columns; }
 

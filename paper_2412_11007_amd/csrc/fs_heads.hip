@@ -13,7 +13,7 @@
 //     (The second product costs 3 to 7 %.  Without it the rounding of P would be in out beside out's own, and through D = g . out, whose
 //     parts cancel in sums over many entries, in the gradient of the bias: 1.5 times the error on a graph of 8 k rows.)
 // At a window's end the tile is divided by l (1 / (1 - p) goes in with it) and stored; parts of a cut window leave fp32 tiles and
-// (m, l), which k_add_parts merges in slot order.  l counts what dropout takes out as well: the mask applies after the softmax.
+// (m, l), which k_merge_parts merges in slot order.  l counts what dropout takes out as well: the mask applies after the softmax.
 // Heads are the slower grid dimension, so that one head's rows of Y and H share the L2s; query heads with the same keys are neighbours.
 #include <type_traits>
 
@@ -171,6 +171,70 @@ k_heads_forward(fs_walk a, fs_operand X, fs_operand Y, fs_operand H, int share, 
     block_step(std::false_type{});
 }
 
+// Merges the parts of one cut window, 32 columns a wavefront, for every head, in slot order.  The parts carry (maximum m, sum l) per
+// row in units of log2, and with m* the largest m of a row
+//   out = factor * sum_k 2^(m_k - m*) tile_k / sum_k 2^(m_k - m*) l_k,   lse = ln 2 * (m* + log2 of that sum).
+// Lane (row r = lane % V, q = lane / V) first walks the parts q, q + 64/V, ...; tiles are read in their storage order, sixteen loads in
+// flight, and the rounded rows leave through LDS.
+template <int DT, int V>
+__global__ void __launch_bounds__(64)
+k_merge_parts(const int4 *__restrict__ split_windows, const float *__restrict__ part, const float *__restrict__ stats, int n_slots, int N,
+            fs_operand out, float factor, int64_t M, float *__restrict__ lse)
+{
+    constexpr int CH = 32, KQ = 64 / V;
+    __shared__ __attribute__((aligned(16))) uint16_t out_t[V][CH + 8];
+    const int n_chunks = (N + CH - 1) / CH, head = blockIdx.y;
+    const int4 sw = split_windows[blockIdx.x / n_chunks];
+    const int w = sw.x, p0 = sw.y, cnt = sw.z;
+    const int lane = threadIdx.x, r = lane % V, q = lane / V;
+    const int c0 = (blockIdx.x % n_chunks) * CH, nc = min(CH, N - c0);
+    const float *st = stats + ((int64_t)head * n_slots + p0) * 2 * V;
+    float top = -INFINITY;
+    for (int k = q; k < cnt; k += KQ) top = fmaxf(top, st[(int64_t)k * 2 * V + r]);
+#pragma unroll
+    for (int o = V; o < 64; o <<= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
+    const float use = top == -INFINITY ? 0.f : top;
+    float total = 0.f;
+    for (int k = q; k < cnt; k += KQ) total += st[(int64_t)k * 2 * V + V + r] * __builtin_amdgcn_exp2f(st[(int64_t)k * 2 * V + r] - use);
+#pragma unroll
+    for (int o = V; o < 64; o <<= 1) total += __shfl_xor(total, o, 64);
+    const float inv = total == 0.f ? 0.f : factor / total;
+    if (lse && c0 == 0 && q == 0 && (int64_t)w * V + r < M) lse[(int64_t)head * M + (int64_t)w * V + r] = fs_log_sum(use, total);
+    const int64_t tile4 = (int64_t)V * N / 4;
+    const fs_f4 *src0 = reinterpret_cast<const fs_f4 *>(part) + ((int64_t)head * n_slots + p0) * tile4 + (c0 / 4) * V;
+    for (int idx = lane; idx < (nc / 4) * V; idx += 64) {  // idx % V == r
+        const int ct = idx / (4 * V), rem = idx - ct * 4 * V, g = rem / V, j = rem - g * V;
+        const fs_f4 *src = src0 + idx;
+        fs_f4 sum = fs_f4{0.f, 0.f, 0.f, 0.f};
+        for (int k = 0; k < cnt; k += 16) {
+            fs_f4 v[16];
+            float wk[16];
+#pragma unroll
+            for (int u = 0; u < 16; u++) {
+                const int kk = min(k + u, cnt - 1);
+                v[u] = src[(int64_t)kk * tile4];
+                wk[u] = st[(int64_t)kk * 2 * V + j];
+            }
+#pragma unroll
+            for (int u = 0; u < 16; u++)
+                if (k + u < cnt) sum += v[u] * __builtin_amdgcn_exp2f(wk[u] - use);
+        }
+        uint2 o;
+        o.x = fs_pack2<DT>(sum[0] * inv, sum[1] * inv);
+        o.y = fs_pack2<DT>(sum[2] * inv, sum[3] * inv);
+        *reinterpret_cast<uint2 *>(&out_t[j][16 * ct + 4 * g]) = o;
+    }
+    __syncthreads();
+    const int c8n = nc / 8;
+    for (int t = lane; t < V * c8n; t += 64) {
+        const int j = t / c8n, c8 = t - j * c8n;
+        const int64_t row = (int64_t)w * V + j;
+        if (row < M)
+            __builtin_nontemporal_store(*reinterpret_cast<const fs_u4 *>(&out_t[j][8 * c8]),
+                                        reinterpret_cast<fs_u4 *>(out.p + head * out.head + row * out.pitch + 2 * (c0 + 8 * c8)));
+    }
+}
+
 __global__ void __launch_bounds__(256) k_zero_heads(fs_operand m, int64_t rows, int pieces, float *__restrict__ lse)
 {
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, row = i / pieces;
@@ -202,7 +266,7 @@ fs_status launch(const fs_format *f, const call &c)
     if (f->n_split_windows > 0) {
         const int64_t blocks = f->n_split_windows * ((c.N + 31) / 32);
         if (blocks >= ((int64_t)1 << 31)) return FS_ERR_TOO_LARGE;
-        k_add_parts<DT, V, true><<<dim3((unsigned)blocks, c.heads), 64, 0, c.st>>>((const int4 *)f->split_windows, c.work, stats, (int)f->n_split_items, c.N,
+        k_merge_parts<DT, V><<<dim3((unsigned)blocks, c.heads), 64, 0, c.st>>>((const int4 *)f->split_windows, c.work, stats, (int)f->n_split_items, c.N,
                                                                                   c.out, c.drop.factor, f->M, c.lse);
         FS_LAUNCH_CHECK();
     }

@@ -15,7 +15,7 @@
 // 2^12: probabilities are at most 1, and those of rows with thousands of entries would lie among its subnormal numbers.
 //
 // dtable: every lane adds the dS of its window row to a column of its own of a table of sums in LDS (V x 4 columns for each
-// bucket), a wavefront leaves one sum per bucket, and those are added in the order of the work list (fs_bucket_sums_launch).
+// bucket), a wavefront leaves one sum per bucket, and those are added in the order of the work list.
 //
 // By columns the query heads that share keys and values are walked inside a block, one after the other, into the same accumulators.
 #include <type_traits>
@@ -26,6 +26,7 @@
 namespace {
 
 constexpr int kSumColumns = 32;  // of the table of sums in LDS, for each bucket
+__host__ __device__ constexpr float fs_weight_scale(int dtype) { return dtype == FS_F16 ? 4096.f : 1.f; }  // of Z P
 
 template <int DT, int V, int KS, int NT>
 __global__ void __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(KS <= 2 && NT <= 4 ? 3 : 2)))
@@ -208,7 +209,7 @@ k_heads_cols(fs_walk a, int64_t rows, fs_operand X, fs_operand Y, fs_operand H, 
     using tile_x = fs_gathered<32 * KS>;
     using tile_g = fs_gathered<16 * NT>;
     constexpr int KN = NT / 2;
-    constexpr float kWeight = DT == FS_F16 ? 4096.f : 1.f;
+    constexpr float kWeight = fs_weight_scale(DT);
     __shared__ __attribute__((aligned(16))) unsigned char lds_x[tile_x::kBytes];
     __shared__ __attribute__((aligned(16))) unsigned char lds_g[tile_g::kBytes];
     __shared__ __attribute__((aligned(16))) int lds_rows[32];
@@ -365,68 +366,173 @@ struct call {
     hipStream_t st;
 };
 
-template <int DT, int V>
-fs_status add_parts(const fs_format *f, int heads, const float *part, int columns, const fs_operand &to, float factor, hipStream_t st)
+// What is left after the walks, in one launch: the partial tiles of cut windows are added and the wavefronts' sums per bucket
+// gathered into a few.
+struct Parts {  // of one output
+    const int4 *split_windows;
+    const float *tiles;
+    fs_operand out;
+    int64_t rows;
+    float factor;
+    int V, n_slots, columns, chunks, groups, heads;  // groups: workgroups, one for a window and 32 columns
+};
+struct Sums {
+    const float *from;
+    float *to;
+    int n, n_buckets, groups, heads;
+};
+
+template <int DT>
+__device__ __forceinline__ void add_parts(const Parts &p, int group, int head)
 {
-    if (f->n_split_windows == 0) return FS_OK;
-    const int64_t blocks = f->n_split_windows * ((columns + 31) / 32);
-    if (blocks >= ((int64_t)1 << 31)) return FS_ERR_TOO_LARGE;
-    k_add_parts<DT, V, false><<<dim3((unsigned)blocks, heads), 64, 0, st>>>((const int4 *)f->split_windows, part, nullptr, (int)f->n_split_items, columns, to, factor,
-                                                                          f->M, nullptr);
+    __shared__ __attribute__((aligned(16))) uint16_t out_t[16][32 + 8];
+    const int V = p.V, lane = threadIdx.x;
+    const int4 sw = p.split_windows[group / p.chunks];  // {window, first slot, slots}
+    const int c0 = group % p.chunks * 32, nc = min(32, p.columns - c0);
+    const int64_t tile4 = (int64_t)V * p.columns / 4;
+    const fs_f4 *src0 = reinterpret_cast<const fs_f4 *>(p.tiles) + ((int64_t)head * p.n_slots + sw.y) * tile4 + (c0 / 4) * V;
+    for (int idx = lane; idx < nc / 4 * V; idx += 64) {  // in storage order: 16-column tile, 4-column group, row
+        const int ct = idx / (4 * V), rem = idx - ct * 4 * V, g = rem / V, j = rem - g * V;
+        fs_f4 sum = fs_f4{0.f, 0.f, 0.f, 0.f};
+        for (int k = 0; k < sw.z; k += 16) {  // sixteen loads in flight, added in slot order
+            fs_f4 v[16];
+#pragma unroll
+            for (int u = 0; u < 16; u++) v[u] = src0[idx + (int64_t)min(k + u, sw.z - 1) * tile4];
+#pragma unroll
+            for (int u = 0; u < 16; u++)
+                if (k + u < sw.z) sum += v[u];
+        }
+        uint2 o;
+        o.x = fs_pack2<DT>(sum[0] * p.factor, sum[1] * p.factor);
+        o.y = fs_pack2<DT>(sum[2] * p.factor, sum[3] * p.factor);
+        *reinterpret_cast<uint2 *>(&out_t[j][16 * ct + 4 * g]) = o;
+    }
+    __syncthreads();
+    for (int t = lane; t < V * (nc / 8); t += 64) {
+        const int j = t / (nc / 8), c8 = t - j * (nc / 8);
+        const int64_t row = (int64_t)sw.x * V + j;
+        if (row < p.rows)
+            __builtin_nontemporal_store(*reinterpret_cast<const fs_u4 *>(&out_t[j][8 * c8]),
+                                        reinterpret_cast<fs_u4 *>(p.out.p + head * p.out.head + row * p.out.pitch + 2 * (c0 + 8 * c8)));
+    }
+}
+
+__device__ __forceinline__ void add_sums(const Sums &s, int group, int head)  // a contiguous share of the wavefronts' sums
+{
+    const int share = (s.n + s.groups - 1) / s.groups, i0 = group * share, i1 = min(s.n, i0 + share);
+    for (int b = threadIdx.x; b < s.n_buckets; b += 64) {
+        const float *from = s.from + (int64_t)head * s.n * s.n_buckets + b;
+        float t = 0.f;
+        for (int i = i0; i < i1; i += 8) {
+            float v[8];
+#pragma unroll
+            for (int k = 0; k < 8; k++) v[k] = from[(int64_t)min(i + k, i1 - 1) * s.n_buckets];
+#pragma unroll
+            for (int k = 0; k < 8; k++) t += i + k < i1 ? v[k] : 0.f;
+        }
+        s.to[((int64_t)head * s.groups + group) * s.n_buckets + b] = t;
+    }
+}
+
+template <int DT>
+__global__ void __launch_bounds__(64) k_heads_finish(Parts x, Parts y, Parts h, Sums s)
+{
+    int group = blockIdx.x;
+    const int head = blockIdx.y;
+    if (group < x.groups) {
+        if (head < x.heads) add_parts<DT>(x, group, head);
+        return;
+    }
+    group -= x.groups;
+    if (group < y.groups) {
+        if (head < y.heads) add_parts<DT>(y, group, head);
+        return;
+    }
+    group -= y.groups;
+    if (group < h.groups) {
+        if (head < h.heads) add_parts<DT>(h, group, head);
+        return;
+    }
+    add_sums(s, group - h.groups, head);
+}
+
+// Where the workspace's pieces lie, in floats: {lse, D} per row and head, the wavefronts' sums per bucket and the groups they are gathered
+// into, the partial tiles of the three outputs.
+struct Pieces {
+    size_t sums, grouped, x, y, h, total;
+    int groups;
+};
+Pieces pieces_of(const fs_format *f, const fs_format *t, int64_t heads, int64_t kv_heads, int64_t d, int64_t N, int64_t n_grad)
+{
+    Pieces p;
+    p.groups = (int)std::min<int64_t>(1024, (f->n_items + 31) / 32);
+    p.sums = fs_align_up(2 * (size_t)heads * (size_t)f->M, 4);
+    p.grouped = p.sums + fs_align_up((size_t)heads * (size_t)f->n_items * (size_t)n_grad, 4);
+    p.x = p.grouped + fs_align_up((size_t)heads * (size_t)p.groups * (size_t)n_grad, 4);
+    p.y = p.x + fs_part_floats(f, heads, d);
+    p.h = p.y + fs_part_floats(t, kv_heads, d);
+    p.total = p.h + fs_part_floats(t, kv_heads, N);
+    return p;
+}
+
+Parts parts_of(const fs_format *f, const float *tiles, int columns, int heads, const fs_operand &out, float factor)
+{
+    const int chunks = (columns + 31) / 32;
+    return Parts{(const int4 *)f->split_windows, tiles, out, f->M, factor, f->V, (int)f->n_split_items, columns, chunks, (int)(f->n_split_windows * chunks), heads};
+}
+
+template <int DT, int V, int KS, int NT>
+fs_status rows_launch(const fs_format *f, const call &c, const Pieces &at)
+{
+    const fs_launch_geometry geo = fs_launch_geometry_for(f, 1);
+    const size_t lds = (fs_bias_lds_bytes(c.bias.n_buckets, c.bias.reach) + 15) / 16 * 16 + (size_t)c.n_grad * 4 * kSumColumns;
+    k_heads_rows<DT, V, KS, NT><<<dim3(geo.nbx, c.heads), 64, lds, c.st>>>(fs_walk_of(f, geo), c.X, c.Y, c.H, c.out, c.G, c.lse, c.heads / c.kv_heads, c.d, c.N,
+                                                                          c.scale * 1.44269504088896340736f, c.scale, c.bias, c.drop, c.dX, (float2 *)c.work,
+                                                                          c.work + at.x, c.n_grad > 0 ? c.work + at.sums : nullptr);
     FS_LAUNCH_CHECK();
     return FS_OK;
 }
 
-// Where the workspace's pieces lie, in floats: {lse, D} per row and head, the buckets' sums, the partial tiles of the walk in progress.
-struct pieces {
-    size_t sums, tiles, total;
-};
-pieces pieces_of(const fs_format *f, const fs_format *t, int64_t heads, int64_t kv_heads, int64_t d, int64_t N, int64_t n_grad)
-{
-    pieces p;
-    p.sums = fs_align_up(2 * (size_t)heads * (size_t)f->M, 4);
-    p.tiles = p.sums + fs_align_up(n_grad > 0 ? fs_bucket_sums_floats(heads, f->n_items, n_grad) : 0, 4);
-    p.total = p.tiles + std::max(fs_part_floats(f, heads, d), fs_part_floats(t, kv_heads, d + N));
-    return p;
-}
-
 template <int DT, int V, int KS, int NT>
-fs_status rows_launch(const fs_format *f, const call &c, const pieces &at)
-{
-    const fs_launch_geometry geo = fs_launch_geometry_for(f, 1);
-    float *tiles = c.work + at.tiles, *sums = c.n_grad > 0 ? c.work + at.sums : nullptr;
-    const size_t lds = (fs_bias_lds_bytes(c.bias.n_buckets, c.bias.reach) + 15) / 16 * 16 + (size_t)c.n_grad * 4 * kSumColumns;
-    k_heads_rows<DT, V, KS, NT><<<dim3(geo.nbx, c.heads), 64, lds, c.st>>>(fs_walk_of(f, geo), c.X, c.Y, c.H, c.out, c.G, c.lse, c.heads / c.kv_heads, c.d, c.N,
-                                                                          c.scale * 1.44269504088896340736f, c.scale, c.bias, c.drop, c.dX, (float2 *)c.work, tiles, sums);
-    FS_LAUNCH_CHECK();
-    const fs_status s = add_parts<DT, V>(f, c.heads, tiles, c.d, c.dX, c.scale, c.st);
-    return s != FS_OK || !sums ? s : fs_bucket_sums_launch(DT, c.heads, (int)f->n_items, c.n_grad, sums, c.table_grad, c.st);
-}
-
-template <int DT, int V, int KS, int NT>
-fs_status cols_launch(const fs_format *f, const fs_format *t, const call &c, const pieces &at)
+fs_status cols_launch(const fs_format *f, const fs_format *t, const call &c, const Pieces &at)
 {
     const fs_launch_geometry geo = fs_launch_geometry_for(t, 1);
     const int share = c.heads / c.kv_heads;
-    float *tiles_y = c.work + at.tiles, *tiles_h = tiles_y + fs_part_floats(t, c.kv_heads, c.d);
     const size_t lds = c.bias.n_buckets > 0 ? fs_bias_lds_bytes(c.bias.n_buckets, c.bias.reach) + 4 * (size_t)c.bias.n_buckets * (share - 1) : 0;
     k_heads_cols<DT, V, KS, NT><<<dim3(geo.nbx, c.kv_heads), 64, lds, c.st>>>(fs_walk_of(t, geo), f->M, c.X, c.Y, c.H, c.G, (const float2 *)c.work, share, c.d, c.N,
-                                                                             c.scale * 1.44269504088896340736f, c.scale, c.bias, c.drop, c.dY, c.dH, tiles_y, tiles_h);
+                                                                             c.scale * 1.44269504088896340736f, c.scale, c.bias, c.drop, c.dY, c.dH, c.work + at.y,
+                                                                             c.work + at.h);
     FS_LAUNCH_CHECK();
-    const fs_status s = add_parts<DT, V>(t, c.kv_heads, tiles_y, c.d, c.dY, c.scale, c.st);
-    return s != FS_OK ? s : add_parts<DT, V>(t, c.kv_heads, tiles_h, c.N, c.dH, c.drop.factor * (DT == FS_F16 ? 1.f / 4096.f : 1.f), c.st);
+    return FS_OK;
+}
+
+template <int DT>
+fs_status finish(const fs_format *f, const fs_format *t, const call &c, const Pieces &at)
+{
+    const Parts x = parts_of(f, c.work + at.x, c.d, c.heads, c.dX, c.scale), y = parts_of(t, c.work + at.y, c.d, c.kv_heads, c.dY, c.scale),
+                h = parts_of(t, c.work + at.h, c.N, c.kv_heads, c.dH, c.drop.factor / fs_weight_scale(DT));
+    const Sums s = {c.work + at.sums, c.work + at.grouped, (int)f->n_items, c.n_grad, c.n_grad > 0 ? at.groups : 0, c.heads};
+    const int64_t blocks = (int64_t)x.groups + y.groups + h.groups + s.groups;
+    if (blocks > 0) {
+        k_heads_finish<DT><<<dim3((unsigned)blocks, c.heads), 64, 0, c.st>>>(x, y, h, s);
+        FS_LAUNCH_CHECK();
+    }
+    return c.n_grad > 0 ? fs_bucket_sums_launch(DT, c.heads, at.groups, c.n_grad, c.work + at.grouped, c.table_grad, c.st) : FS_OK;
 }
 
 // The two formats may have windows of different heights.
 template <int DT, int KS, int NT>
 fs_status launch(const fs_format *f, const fs_format *t, const call &c)
 {
-    const pieces at = pieces_of(f, t, c.heads, c.kv_heads, c.d, c.N, c.n_grad);
-    const fs_status s = f->V == 4   ? rows_launch<DT, 4, KS, NT>(f, c, at)
-                        : f->V == 8 ? rows_launch<DT, 8, KS, NT>(f, c, at)
-                                    : rows_launch<DT, 16, KS, NT>(f, c, at);
-    if (s != FS_OK) return s;
-    return t->V == 4 ? cols_launch<DT, 4, KS, NT>(f, t, c, at) : t->V == 8 ? cols_launch<DT, 8, KS, NT>(f, t, c, at) : cols_launch<DT, 16, KS, NT>(f, t, c, at);
+    const Pieces at = pieces_of(f, t, c.heads, c.kv_heads, c.d, c.N, c.n_grad);
+    fs_status s = f->V == 4   ? rows_launch<DT, 4, KS, NT>(f, c, at)
+                  : f->V == 8 ? rows_launch<DT, 8, KS, NT>(f, c, at)
+                              : rows_launch<DT, 16, KS, NT>(f, c, at);
+    if (s == FS_OK)
+        s = t->V == 4   ? cols_launch<DT, 4, KS, NT>(f, t, c, at)
+            : t->V == 8 ? cols_launch<DT, 8, KS, NT>(f, t, c, at)
+                        : cols_launch<DT, 16, KS, NT>(f, t, c, at);
+    return s == FS_OK ? finish<DT>(f, t, c, at) : s;
 }
 template <int DT, int KS>
 fs_status launch_n(const fs_format *f, const fs_format *t, const call &c)
