@@ -156,7 +156,9 @@ def load_library():
     _fs_torch.bind(*(ctypes.cast(f, vp).value for f in (
         lib.fs_spmm_workspace_bytes, lib.fs_attention_workspace_bytes, lib.fs_edge_softmax_workspace_bytes, lib.fs_spmm,
         lib.fs_sddmm, lib.fs_attention, lib.fs_sddmm_spmm, lib.fs_edge_softmax, lib.fs_edge_softmax_backward,
-        lib.fs_csr_to_blk, lib.fs_blk_to_csr, lib.fs_gather16)))
+        lib.fs_csr_to_blk, lib.fs_blk_to_csr, lib.fs_gather16, lib.fs_edge_bias, lib.fs_edge_bias_backward_workspace_bytes,
+        lib.fs_edge_bias_backward, lib.fs_edge_dropout, lib.fs_attention_forward_workspace_bytes, lib.fs_attention_forward,
+        lib.fs_attention_backward_workspace_bytes, lib.fs_attention_backward)))
     _lib, _native = lib, _fs_torch
     return lib
 
@@ -626,6 +628,10 @@ def _value_heads(fmt, vals):
 
 def fs_edge_bias(fmt: FsFormat, vals, bias: FsBucketBias, scale: float = 1.0, out=None, stream=None):
     """scale * value + the bias of the entry, on vals_blk-layout arrays, one or (heads, V*nvec) (out may be vals)."""
+    if out is None:
+        got = _calls().edge_bias(ctypes.addressof(fmt.c), vals, bias.table, bias.buckets, bias.shift, scale, _stream_ptr(stream))
+        if got is not None:
+            return _result(got, "fs_edge_bias")
     heads = _value_heads(fmt, vals)
     if out is None:
         out = torch.empty_like(vals)
@@ -648,6 +654,10 @@ def fs_edge_bias_backward_workspace_bytes(fmt: FsFormat, heads: int, n_buckets: 
 def fs_edge_bias_backward(fmt: FsFormat, grad, bias: FsBucketBias, out=None, work=None, stream=None):
     """Gradient of the bias table from the gradient of fs_edge_bias's result (the gradient of its values is scale * grad):
     (heads, buckets), or (buckets,) for a single array."""
+    if out is None and work is None:
+        got = _calls().edge_bias_backward(ctypes.addressof(fmt.c), grad, bias.table, bias.buckets, bias.shift, stream, _stream_ptr(stream))
+        if got is not None:
+            return _result(got, "fs_edge_bias_backward")
     heads = _value_heads(fmt, grad)
     n_buckets = bias.table.shape[-1]
     if out is None:
@@ -665,6 +675,10 @@ def fs_edge_bias_backward(fmt: FsFormat, grad, bias: FsBucketBias, out=None, wor
 def fs_edge_dropout(fmt: FsFormat, vals, dropout: FsDropout, out=None, stream=None):
     """Dropout on vals_blk-layout arrays, one or (heads, V*nvec): the probabilities in the forward pass, their gradient in the
     backward pass (out may be vals)."""
+    if out is None:
+        got = _calls().edge_dropout(ctypes.addressof(fmt.c), vals, dropout.state, dropout.p, _stream_ptr(stream))
+        if got is not None:
+            return _result(got, "fs_edge_dropout")
     heads = _value_heads(fmt, vals)
     if out is None:
         out = torch.empty_like(vals)
@@ -681,6 +695,14 @@ def _head_matrix(t, fmt, rows):
     heads, columns = (t.shape[1], t.shape[2]) if t.dim() == 3 else (1, t.shape[1])
     return (_FsHeadMatrix(t.data_ptr(), t.stride(0) if rows > 1 else max(t.stride(0), columns), t.stride(1) if heads > 1 else 0 if t.dim() == 2 else columns),
             heads, columns)
+
+
+def _bias_args(bias):
+    return (None, None, 0) if bias is None else (bias.table, bias.buckets, bias.shift)
+
+
+def _dropout_args(dropout):
+    return (None, 0.0) if dropout is None else (dropout.state, dropout.p)
 
 
 def fs_attention_forward_workspace_bytes(fmt: FsFormat, heads: int, N: int) -> int:
@@ -706,6 +728,10 @@ def fs_attention_forward(fmt: FsFormat, X, Y, H, scale: float = 1.0, bias: Optio
 
     X: (M, d) or (M, heads, d); Y: (K, d) or (K, kv_heads, d), H the same with N columns; a query head h reads
     keys and values h // (heads // kv_heads).  Returns (out, lse): like X with N columns, and float32 (M,) or (heads, M)."""
+    if out is None and lse is None and work is None:
+        got = _calls().attention_forward(ctypes.addressof(fmt.c), X, Y, H, scale, *_bias_args(bias), *_dropout_args(dropout), stream, _stream_ptr(stream))
+        if got is not None:
+            return _result(got, "fs_attention_forward")
     heads, kv_heads, d, N, x, y, h, b, dr = _attention_operands(fmt, X, Y, H, bias, dropout)
     M = fmt.c.M
     if out is None:
@@ -736,6 +762,11 @@ def fs_attention_backward(fmt: FsFormat, fmt_t: FsFormat, X, Y, H, out, lse, gra
                           dropout: Optional[FsDropout] = None, dX=None, dY=None, dH=None, dTable=None, work=None, stream=None):
     """The gradients of fs_attention_forward, whose ``out`` and ``lse`` these are, from the gradient ``grad`` of out: (dX, dY, dH,
     dTable), the last None without a bias.  ``fmt_t`` is the format of A^T (fs_csr_transpose, fs_convert)."""
+    if dX is None and dY is None and dH is None and dTable is None and work is None:
+        got = _calls().attention_backward(ctypes.addressof(fmt.c), ctypes.addressof(fmt_t.c), X, Y, H, out, lse, grad, scale, *_bias_args(bias),
+                                          *_dropout_args(dropout), stream, _stream_ptr(stream))
+        if got is not None:
+            return _result(got, "fs_attention_backward")
     heads, kv_heads, d, N, x, y, h, b, dr = _attention_operands(fmt, X, Y, H, bias, dropout)
     M = fmt.c.M
     assert out.dim() == grad.dim() == X.dim()

@@ -9,6 +9,9 @@
 // the binding's checks in Python then name.
 #include <Python.h>
 
+#include <algorithm>
+#include <initializer_list>
+
 #include <ATen/core/Tensor.h>
 #include <ATen/ops/empty.h>
 #include <c10/core/StreamGuard.h>
@@ -34,6 +37,14 @@ struct Entry {
     decltype(&fs_csr_to_blk) csr_to_blk;
     decltype(&fs_blk_to_csr) blk_to_csr;
     decltype(&fs_gather16) gather16;
+    decltype(&fs_edge_bias) edge_bias;
+    decltype(&fs_edge_bias_backward_workspace_bytes) edge_bias_backward_work;
+    decltype(&fs_edge_bias_backward) edge_bias_backward;
+    decltype(&fs_edge_dropout) edge_dropout;
+    decltype(&fs_attention_forward_workspace_bytes) attention_forward_work;
+    decltype(&fs_attention_forward) attention_forward;
+    decltype(&fs_attention_backward_workspace_bytes) attention_backward_work;
+    decltype(&fs_attention_backward) attention_backward;
 } g;
 constexpr Py_ssize_t kEntries = sizeof(Entry) / sizeof(void *);
 
@@ -200,6 +211,205 @@ FS_ENTRY(blk_to_csr, 3)  // format, values in vals_blk layout, stream
     return finish(out, st);
 FS_ENTRY_END
 
+// (rows, columns) or (rows, heads, columns)
+struct Heads {
+    fs_head_matrix m;
+    int64_t heads = 0, columns = 0;
+    bool ok = false;
+    Heads(PyObject *o, const fs_format *f, int64_t rows)
+    {
+        if (!THPVariable_Check(o)) return;
+        const at::Tensor &t = THPVariable_Unpack(o);
+        set(t, f, rows);
+    }
+    Heads(const at::Tensor &t, const fs_format *f, int64_t rows) { set(t, f, rows); }
+    void set(const at::Tensor &t, const fs_format *f, int64_t rows)
+    {
+        const int64_t dim = t.dim();
+        if ((dim != 2 && dim != 3) || !of_format(t, f) || t.size(0) != rows || t.stride(dim - 1) != 1) return;
+        heads = dim == 3 ? t.size(1) : 1;
+        columns = t.size(dim - 1);
+        m.d = t.data_ptr();
+        m.ld = rows > 1 ? t.stride(0) : std::max(t.stride(0), columns);
+        m.head = heads > 1 ? t.stride(1) : dim == 2 ? 0 : columns;
+        ok = true;
+    }
+};
+
+// table or None, buckets, shift: three arguments
+struct Bias {
+    fs_bucket_bias b = {};
+    bool given = false, ok = true;
+    Bias(PyObject *const *a, const fs_format *f, int64_t heads)
+    {
+        if (a[0] == Py_None) return;
+        given = true;
+        ok = false;
+        if (!THPVariable_Check(a[0]) || !THPVariable_Check(a[1])) return;
+        const at::Tensor &t = THPVariable_Unpack(a[0]), &k = THPVariable_Unpack(a[1]);
+        if (!k.is_cuda() || k.scalar_type() != at::kByte || !k.is_contiguous() || k.numel() % 2 != 1 || k.numel() > (1 << 30)) return;
+        if ((t.dim() != 1 && t.dim() != 2) || !of_format(t, f) || t.stride(-1) != 1 || (t.dim() == 2 ? t.size(0) : 1) != heads) return;
+        b.d_table = t.data_ptr();
+        b.n_buckets = (int32_t)t.size(-1);
+        b.ld = t.dim() == 2 && heads > 1 ? t.stride(0) : b.n_buckets;
+        b.d_bucket = (const uint8_t *)k.data_ptr();
+        b.reach = (int32_t)(k.numel() / 2);
+        b.shift = PyLong_AsLongLong(a[2]);
+        ok = !PyErr_Occurred();
+    }
+    const fs_bucket_bias *get() const { return given ? &b : nullptr; }
+};
+
+// state or None, p: two arguments
+struct Dropout {
+    fs_dropout d = {};
+    bool given = false, ok = true;
+    explicit Dropout(PyObject *const *a)
+    {
+        if (a[0] == Py_None) return;
+        given = true;
+        ok = false;
+        if (!THPVariable_Check(a[0])) return;
+        const at::Tensor &s = THPVariable_Unpack(a[0]);
+        if (!s.is_cuda() || s.scalar_type() != at::kLong || !s.is_contiguous() || s.numel() != 2) return;
+        d.d_state = (const int64_t *)s.data_ptr();
+        d.p = PyFloat_AsDouble(a[1]);
+        ok = !PyErr_Occurred();
+    }
+    const fs_dropout *get() const { return given ? &d : nullptr; }
+};
+
+// Value arrays, one or (heads, V * nvec).
+bool value_arrays(PyObject *o, const fs_format *f, int64_t *heads)
+{
+    if (!THPVariable_Check(o)) return false;
+    const at::Tensor &t = THPVariable_Unpack(o);
+    if ((t.dim() != 1 && t.dim() != 2) || !of_format(t, f) || !t.is_contiguous() || t.size(-1) != f->V * f->nvec) return false;
+    *heads = t.dim() == 2 ? t.size(0) : 1;
+    return *heads < (1 << 30);
+}
+
+FS_ENTRY(edge_bias, 7)  // format, values, table, buckets, shift, scale, stream
+    int64_t heads = 0;
+    if (!value_arrays(a[1], f, &heads)) Py_RETURN_NONE;
+    const Bias bias(a + 2, f, heads);
+    const float scale = (float)PyFloat_AsDouble(a[5]);
+    if (PyErr_Occurred()) return nullptr;
+    if (!bias.ok) Py_RETURN_NONE;
+    const at::Tensor &v = THPVariable_Unpack(a[1]);
+    at::Tensor out = at::empty(v.sizes(), v.options());
+    FS_CALL(st, g.edge_bias(f, (int32_t)heads, v.data_ptr(), scale, bias.get(), out.data_ptr(), stream))
+    return finish(out, st);
+FS_ENTRY_END
+
+FS_ENTRY(edge_bias_backward, 7)  // format, gradient, table, buckets, shift, stream object, stream
+    int64_t heads = 0;
+    if (!value_arrays(a[1], f, &heads) || !stream_or_none(a[5])) Py_RETURN_NONE;
+    const Bias bias(a + 2, f, heads);
+    if (PyErr_Occurred()) return nullptr;
+    if (!bias.ok || !bias.given) Py_RETURN_NONE;
+    const at::Tensor &v = THPVariable_Unpack(a[1]);
+    at::Tensor out = v.dim() == 2 ? at::empty({heads, (int64_t)bias.b.n_buckets}, v.options()) : at::empty({(int64_t)bias.b.n_buckets}, v.options());
+    size_t bytes = 0;
+    st = g.edge_bias_backward_work(f, (int32_t)heads, bias.b.n_buckets, &bytes);
+    if (st != FS_OK) return finish(out, st);
+    at::Tensor work = temporary_on(v, (int64_t)bytes, a[5]);
+    FS_CALL(st, g.edge_bias_backward(f, (int32_t)heads, v.data_ptr(), bias.get(), out.data_ptr(), work.data_ptr(), bytes, stream))
+    return finish(out, st);
+FS_ENTRY_END
+
+FS_ENTRY(edge_dropout, 5)  // format, values, state, p, stream
+    int64_t heads = 0;
+    if (!value_arrays(a[1], f, &heads)) Py_RETURN_NONE;
+    const Dropout drop(a + 2);
+    if (PyErr_Occurred()) return nullptr;
+    if (!drop.ok || !drop.given) Py_RETURN_NONE;
+    const at::Tensor &v = THPVariable_Unpack(a[1]);
+    at::Tensor out = at::empty(v.sizes(), v.options());
+    FS_CALL(st, g.edge_dropout(f, (int32_t)heads, v.data_ptr(), drop.get(), out.data_ptr(), stream))
+    return finish(out, st);
+FS_ENTRY_END
+
+// X, Y, H of a call with heads: whether they go together, and the heads fit an int.
+bool go_together(const Heads &x, const Heads &y, const Heads &h, PyObject *const *a)
+{
+    if (!x.ok || !y.ok || !h.ok) return false;
+    const int64_t dim = THPVariable_Unpack(a[0]).dim();
+    return x.columns == y.columns && y.heads == h.heads && THPVariable_Unpack(a[1]).dim() == dim &&
+           THPVariable_Unpack(a[2]).dim() == dim && x.heads < (1 << 30) && y.heads < (1 << 30);
+}
+
+PyObject *none()
+{
+    Py_INCREF(Py_None);
+    return Py_None;
+}
+
+PyObject *tuple_of(std::initializer_list<const at::Tensor *> ts)  // (null: None)
+{
+    PyObject *out = PyTuple_New((Py_ssize_t)ts.size());
+    Py_ssize_t i = 0;
+    for (const at::Tensor *t : ts) {
+        PyObject *o = t ? THPVariable_Wrap(*t) : none();
+        if (!out || !o) {
+            Py_XDECREF(out);
+            Py_XDECREF(o);
+            return nullptr;
+        }
+        PyTuple_SET_ITEM(out, i++, o);
+    }
+    return out;
+}
+
+FS_ENTRY(attention_forward, 12)  // format, X, Y, H, scale, table, buckets, shift, state, p, stream object, stream
+    const Heads x(a[1], f, f->M), y(a[2], f, f->K), h(a[3], f, f->K);
+    if (!go_together(x, y, h, a + 1) || !stream_or_none(a[10])) Py_RETURN_NONE;
+    const float scale = (float)PyFloat_AsDouble(a[4]);
+    const Bias bias(a + 5, f, x.heads);
+    const Dropout drop(a + 8);
+    if (PyErr_Occurred()) return nullptr;
+    if (!bias.ok || !drop.ok) Py_RETURN_NONE;
+    const at::Tensor &X = THPVariable_Unpack(a[1]);
+    const bool flat_ = X.dim() == 2;
+    at::Tensor out = flat_ ? at::empty({f->M, h.columns}, X.options()) : at::empty({f->M, x.heads, h.columns}, X.options());
+    at::Tensor lse = flat_ ? at::empty({f->M}, X.options().dtype(at::kFloat)) : at::empty({x.heads, f->M}, X.options().dtype(at::kFloat));
+    Work w(f, X, a[10], [&](size_t *b) { return g.attention_forward_work(f, (int32_t)x.heads, h.columns, b); });
+    if (w.st != FS_OK) return finish(out, w.st);
+    const Heads o(out, f, f->M);
+    FS_CALL(st, g.attention_forward(f, (int32_t)x.heads, (int32_t)y.heads, x.columns, h.columns, scale, &x.m, &y.m, &h.m, bias.get(), drop.get(), &o.m,
+                                    (float *)lse.data_ptr(), w.p, w.bytes, stream))
+    return st == FS_OK ? tuple_of({&out, &lse}) : PyLong_FromLong((long)st);
+FS_ENTRY_END
+
+// format, format of A^T, X, Y, H, out, lse, gradient of out, scale, table, buckets, shift, state, p, stream object, stream
+FS_ENTRY(attention_backward, 16)
+    const fs_format *ft = format_at(a[1]);
+    if (PyErr_Occurred()) return nullptr;
+    const Heads x(a[2], f, f->M), y(a[3], f, f->K), h(a[4], f, f->K), o(a[5], f, f->M), go(a[7], f, f->M);
+    if (!o.ok || !go.ok || !go_together(x, y, h, a + 2) || o.heads != x.heads || go.heads != x.heads || o.columns != h.columns || go.columns != h.columns ||
+        !stream_or_none(a[14]) || !THPVariable_Check(a[6]))
+        Py_RETURN_NONE;
+    const at::Tensor &X = THPVariable_Unpack(a[2]), &Y = THPVariable_Unpack(a[3]), &H = THPVariable_Unpack(a[4]), &lse = THPVariable_Unpack(a[6]);
+    if (THPVariable_Unpack(a[5]).dim() != X.dim() || THPVariable_Unpack(a[7]).dim() != X.dim() || !lse.is_cuda() || lse.scalar_type() != at::kFloat ||
+        lse.numel() != x.heads * f->M || !lse.is_contiguous())
+        Py_RETURN_NONE;
+    const float scale = (float)PyFloat_AsDouble(a[8]);
+    const Bias bias(a + 9, f, x.heads);
+    const Dropout drop(a + 12);
+    if (PyErr_Occurred()) return nullptr;
+    if (!bias.ok || !drop.ok) Py_RETURN_NONE;
+    at::Tensor dX = at::empty(X.sizes(), X.options()), dY = at::empty(Y.sizes(), Y.options()), dH = at::empty(H.sizes(), H.options()), dT;
+    if (bias.given) dT = at::empty(THPVariable_Unpack(a[9]).sizes(), X.options());
+    size_t bytes = 0;
+    st = g.attention_backward_work(f, ft, (int32_t)x.heads, (int32_t)y.heads, x.columns, h.columns, bias.given ? bias.b.n_buckets : 0, &bytes);
+    if (st != FS_OK) return finish(dX, st);
+    at::Tensor work = temporary_on(X, (int64_t)bytes, a[14]);
+    const Heads mx(dX, f, f->M), my(dY, f, f->K), mh(dH, f, f->K);
+    FS_CALL(st, g.attention_backward(f, ft, (int32_t)x.heads, (int32_t)y.heads, x.columns, h.columns, scale, &x.m, &y.m, &h.m, bias.get(), drop.get(), &o.m,
+                                     (const float *)lse.data_ptr(), &go.m, &mx.m, &my.m, &mh.m, bias.given ? dT.data_ptr() : nullptr, work.data_ptr(), bytes, stream))
+    return st == FS_OK ? tuple_of({&dX, &dY, &dH, bias.given ? &dT : nullptr}) : PyLong_FromLong((long)st);
+FS_ENTRY_END
+
 PyObject *gather16(PyObject *, PyObject *const *a, Py_ssize_t n)  // source, indices, stream
 {
     HANDLE_TH_ERRORS
@@ -245,6 +455,8 @@ PyObject *holds16(PyObject *, PyObject *const *a, Py_ssize_t n)  // a tensor; do
 #define FS_METHOD(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FS_METHOD(bind), FS_METHOD(spmm), FS_METHOD(sddmm), FS_METHOD(attention), FS_METHOD(softmax),
                          FS_METHOD(softmax_backward), FS_METHOD(csr_to_blk), FS_METHOD(blk_to_csr), FS_METHOD(gather16),
+                         FS_METHOD(edge_bias), FS_METHOD(edge_bias_backward), FS_METHOD(edge_dropout),
+                         FS_METHOD(attention_forward), FS_METHOD(attention_backward),
                          FS_METHOD(temporary), FS_METHOD(holds16),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_fs_torch", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
