@@ -49,6 +49,14 @@ __host__ __device__ __forceinline__ fs_key fs_threefry(fs_key key, uint32_t c0, 
     return fs_key{a, b};
 }
 
+// The lane's number as something that is not known ahead of a loop: addresses that only a window's end needs are worked out there, where they
+// would be kept over all blocks otherwise, in registers that spill (and a spilled register's load waits for the gathers before it).
+__device__ __forceinline__ int fs_lane_here(int lane)
+{
+    asm volatile("" : "+v"(lane));
+    return lane;
+}
+
 // What the kernels are given of a bias and of a dropout (n_buckets = 0, state null: none).
 struct fs_bias_args {
     const uint16_t *table;
@@ -246,8 +254,9 @@ struct fs_gathered {
 // A window's rows in operand layout: lane (j, g) holds columns 32ks + 8g .. +7 of row w * V + j; rows past V or the last, and columns
 // past `width`, are zeros.  Lanes without a row load nothing: in this layout a load takes the vector-memory unit a cycle per lane.
 template <int V, int STEPS>
-__device__ __forceinline__ void fs_load_window(fs_frag (&held)[STEPS], const unsigned char *base, uint32_t pitch, int width, int w, int64_t rows, int lane)
+__device__ __forceinline__ void fs_load_window(fs_frag (&held)[STEPS], const unsigned char *base, uint32_t pitch, int width, int w, int64_t rows, int lane_)
 {
+    const int lane = fs_lane_here(lane_);
     const int j = lane & 15, g = lane >> 4;
     const int64_t row = (int64_t)w * V + j;
 #pragma unroll
@@ -287,8 +296,9 @@ struct fs_entries {
     float value[V * kPitch] __attribute__((aligned(16)));
 
     // m: occupancy of row j.  Returns how many of the list's elements to take, the same in all lanes.
-    __device__ __forceinline__ int make_list(uint32_t m, int lane)
+    __device__ __forceinline__ int make_list(uint32_t m, int lane_)
     {
+        const int lane = fs_lane_here(lane_);
         const int j = lane & 15, g = lane >> 4;
         const int own = __popc(m);
         int sum = own;  // over the rows up to j
@@ -409,9 +419,10 @@ __device__ __forceinline__ fs_frag fs_round8_rest(const float (&p)[8], const fs_
 // Accumulators -> rounded rows of an output of up to NC columns, by way of the tile's LDS.
 template <int DT, int V, int NC>
 __device__ __forceinline__ void fs_store_window(unsigned char *lds, const fs_f4 (&acc)[NC / 16], float factor, unsigned char *base, uint32_t pitch,
-                                                int width, int w, int64_t rows, int lane)
+                                                int width, int w, int64_t rows, int lane_)
 {
     using tile = fs_gathered<NC>;
+    const int lane = fs_lane_here(lane_);
     FS_WAVE_SYNC();
     fs_round_tile_to_lds<DT, V, NC / 16, tile::RS>(lds, acc, lane & 15, lane >> 4, factor);
     FS_WAVE_SYNC();
@@ -422,8 +433,9 @@ __device__ __forceinline__ void fs_store_window(unsigned char *lds, const fs_f4 
 
 // Accumulators -> partial tile `slot` of a head's tiles of `width` columns.
 template <int V, int NT>
-__device__ __forceinline__ void fs_store_part(float *tiles, int slot, int width, const fs_f4 (&acc)[NT], int lane)
+__device__ __forceinline__ void fs_store_part(float *tiles, int slot, int width, const fs_f4 (&acc)[NT], int lane_)
 {
+    const int lane = fs_lane_here(lane_);
     const int j = lane & 15, g = lane >> 4;
     fs_store_partial_tile<V, NT>(tiles, slot, width, (uint32_t)((g * V + j) * 16), acc, j < V, NT * 16 <= width, 0, g);
 }

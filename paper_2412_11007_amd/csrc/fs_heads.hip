@@ -23,7 +23,7 @@
 namespace {
 
 template <int DT, int V, int KS, int NT>
-__global__ void __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(NT == 8 && KS > 1 ? 2 : 3)))
+__global__ void __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(KS <= 2 && NT <= 4 ? 4 : KS > 1 && NT == 8 ? 2 : 3)))
 k_heads_forward(fs_walk a, fs_operand X, fs_operand Y, fs_operand H, int share, int d, int N, float sl2, fs_bias_args bias, fs_drop_args drop,
                 fs_operand out, float *__restrict__ lse, float *__restrict__ part, float *__restrict__ stats)
 {
@@ -94,7 +94,6 @@ k_heads_forward(fs_walk a, fs_operand X, fs_operand Y, fs_operand H, int share, 
         if (MORE && d1.w != d0.w) fs_load_window<V>(xf, Xb, X.pitch, d, d1.w, a.M, lane);
         if constexpr (MORE) h.load(Hb, H.pitch, h_colb, cols1, lane);
         FS_WAVE_SYNC();
-        const int row = d0.w * V + j;
         const uint32_t m8 = bits0 >> (8 * g);
         float p[8], mx = -INFINITY;
         uint32_t kept[8];
@@ -144,6 +143,7 @@ k_heads_forward(fs_walk a, fs_operand X, fs_operand Y, fs_operand H, int share, 
         if (d0.last || !MORE) {
             float l_tot = l_run + __shfl_xor(l_run, 16, 64);
             l_tot += __shfl_xor(l_tot, 32, 64);
+            const int l = fs_lane_here(lane), j = l & 15, g = l >> 4, row = d0.w * V + j;
             if (d0.last && from_first) {
                 fs_store_window<DT, V, 16 * NT>(lds, acc, l_tot == 0.f ? 0.f : drop.factor / l_tot, out.p + head * out.head, out.pitch, N, d0.w, a.M, lane);
                 if (lse && g == 0 && j < V && row < a.M) lse[(int64_t)head * a.M + row] = fs_log_sum(m_run, l_tot);

@@ -29,7 +29,7 @@ constexpr int kSumColumns = 32;  // of the table of sums in LDS, for each bucket
 __host__ __device__ constexpr float fs_weight_scale(int dtype) { return dtype == FS_F16 ? 4096.f : 1.f; }  // of Z P
 
 template <int DT, int V, int KS, int NT>
-__global__ void __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(KS <= 2 && NT <= 4 ? 3 : 2)))
+__global__ void __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(KS * NT <= 4 ? 4 : KS <= 2 && NT <= 4 ? 3 : 2)))
 k_heads_rows(fs_walk a, fs_operand X, fs_operand Y, fs_operand H, fs_operand out, fs_operand G, const float *__restrict__ lse, int share, int d, int N,
              float sl2, float scale, fs_bias_args bias, fs_drop_args drop, fs_operand dX, float2 *__restrict__ row_stats, float *__restrict__ part,
              float *__restrict__ bucket_sums)
@@ -77,6 +77,7 @@ k_heads_rows(fs_walk a, fs_operand X, fs_operand Y, fs_operand H, fs_operand out
         fs_load_window<V>(xf, Xb, X.pitch, d, w, a.M, lane);
         fs_load_window<V>(gf, Gb, G.pitch, N, w, a.M, lane);
         fs_load_window<V>(of, Ob, out.pitch, N, w, a.M, lane);
+        const int j = fs_lane_here(lane) & 15;
         const int64_t row = (int64_t)w * V + j;
         if (j < V && row < a.M) my_lse = lse[(int64_t)head * a.M + row];
     };
@@ -115,8 +116,8 @@ k_heads_rows(fs_walk a, fs_operand X, fs_operand Y, fs_operand H, fs_operand out
         }
         h.put(lds, lane, N);
         if constexpr (MORE) h.load(Hb, H.pitch, h_colb, cols1, lane);
-        const int row = d0.w * V + j;
         if (new_window) {
+            const int j = fs_lane_here(lane) & 15, row = d0.w * V + j;
             D = 0.f;
 #pragma unroll
             for (int ks = 0; ks < KN; ks++)
@@ -201,7 +202,7 @@ k_heads_rows(fs_walk a, fs_operand X, fs_operand Y, fs_operand H, fs_operand out
 
 // By columns: `a` walks A^T, its vectors are rows of A (`rows` of them) and its window rows columns.
 template <int DT, int V, int KS, int NT>
-__global__ void __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(KS * NT <= 8 ? 3 : 2)))
+__global__ void __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(KS <= 2 && NT <= 4 ? 3 : 2)))
 k_heads_cols(fs_walk a, int64_t rows, fs_operand X, fs_operand Y, fs_operand H, fs_operand G, const float2 *__restrict__ row_stats, int share, int d,
              int N, float sl2, float scale, fs_bias_args bias, fs_drop_args drop, fs_operand dY, fs_operand dH, float *__restrict__ part_y,
              float *__restrict__ part_h)
