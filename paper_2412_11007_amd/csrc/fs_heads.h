@@ -275,6 +275,10 @@ __device__ __forceinline__ int fs_block_cols(const fs_walk &a, const BlockDesc &
     return a.vec_col[max(min(b.s + min(lane & 31, b.kb - 1), a.nvec - 1), 0)];
 }
 
+// The same for the first block of an item, whose first vector stands in the item's record: beside its descriptor, not after it.  Vectors
+// past its width are the next block's, whose products nobody reads.
+__device__ __forceinline__ int fs_first_cols(const fs_walk &a, const int4 &item, int lane) { return a.vec_col[min(item.w + (lane & 31), a.nvec - 1)]; }
+
 // Occupancy of window row j in block i of an item: bit c, the row stores the block's vector c (none for lanes past V).
 template <int V>
 __device__ __forceinline__ uint32_t fs_row_bits(const fs_walk &a, int first_slot, int i, int nblk, int lane)
@@ -296,8 +300,9 @@ struct fs_entries {
     float value[V * kPitch] __attribute__((aligned(16)));
 
     // m: occupancy of row j.  Returns how many of the list's elements to take, the same in all lanes.
-    __device__ __forceinline__ int make_list(uint32_t m, int lane_)
+    __device__ __forceinline__ int make_list(uint32_t m, int lane_, bool draws)
     {
+        if (V == 4 || (V == 8 && !draws)) return 32 * V;
         const int lane = fs_lane_here(lane_);
         const int j = lane & 15, g = lane >> 4;
         const int own = __popc(m);

@@ -40,6 +40,12 @@ k_heads_forward(fs_walk a, fs_operand X, fs_operand Y, fs_operand H, int share, 
     const int turn = __builtin_amdgcn_readfirstlane(fs_launch_turn<1>(blockIdx.x, a.slice, a.n_swz));
     if (turn >= a.n_items) return;
     const int4 it = a.items[turn];
+    // while the item is on its way: what does not depend on it
+    if (bias.n_buckets > 0) {
+        fs_load_buckets(bias, lut, lane, 64);
+        for (int i = lane; i < bias.n_buckets; i += 64) table[i] = fs_flagless_log2(fs_widen<DT>(bias.table[head * bias.ld + i]));
+    }
+    const fs_key key = fs_drop_key(drop, head);
     const int nblk = it.y;
     if (nblk == 0) return;
     int slot = it.z;
@@ -50,7 +56,7 @@ k_heads_forward(fs_walk a, fs_operand X, fs_operand Y, fs_operand H, int share, 
     const uint32_t y_colb = tile_y::column_bytes(lane, d), h_colb = tile_h::column_bytes(lane, N);
 
     BlockDesc d0 = block(0), d1 = block(1);
-    int cols0 = fs_block_cols(a, d0, lane), cols1 = fs_block_cols(a, d1, lane);
+    int cols0 = fs_first_cols(a, it, lane), cols1 = fs_block_cols(a, d1, lane);
     uint32_t bits0 = fs_row_bits<V>(a, it.x, 0, nblk, lane);
     fs_frag xf[KS];
     fs_load_window<V>(xf, Xb, X.pitch, d, d0.w, a.M, lane);
@@ -58,11 +64,6 @@ k_heads_forward(fs_walk a, fs_operand X, fs_operand Y, fs_operand H, int share, 
     tile_h h;
     y.load(Yb, Y.pitch, y_colb, cols0, lane);
     h.load(Hb, H.pitch, h_colb, cols0, lane);
-    if (bias.n_buckets > 0) {
-        fs_load_buckets(bias, lut, lane, 64);
-        for (int i = lane; i < bias.n_buckets; i += 64) table[i] = fs_flagless_log2(fs_widen<DT>(bias.table[head * bias.ld + i]));
-    }
-    const fs_key key = fs_drop_key(drop, head);
 
     const bool looks_up = bias.n_buckets > 0 || drop.state;
 
@@ -82,7 +83,7 @@ k_heads_forward(fs_walk a, fs_operand X, fs_operand Y, fs_operand H, int share, 
             bits1 = fs_row_bits<V>(a, it.x, step + 1, nblk, lane);
         }
         FS_WAVE_SYNC();
-        if (looks_up) entries.template look_up<false>(entries.make_list(bits0, lane), lane, d0.w * V, cols0, lds_cols, bias, table, lut, drop, key);
+        if (looks_up) entries.template look_up<false>(entries.make_list(bits0, lane, drop.state), lane, d0.w * V, cols0, lds_cols, bias, table, lut, drop, key);
         y.put(lds, lane, d);
         if constexpr (MORE) y.load(Yb, Y.pitch, y_colb, cols1, lane);
         FS_WAVE_SYNC();

@@ -49,6 +49,12 @@ k_heads_rows(fs_walk a, fs_operand X, fs_operand Y, fs_operand H, fs_operand out
     const int turn = __builtin_amdgcn_readfirstlane(fs_launch_turn<1>(blockIdx.x, a.slice, a.n_swz));
     if (turn >= a.n_items) return;
     const int4 it = a.items[turn];
+    // while the item is on its way: what does not depend on it
+    if (bias.n_buckets > 0) {
+        fs_load_buckets(bias, lut, lane, 64);
+        for (int i = lane; i < bias.n_buckets; i += 64) table[i] = fs_flagless_log2(fs_widen<DT>(bias.table[head * bias.ld + i]));
+    }
+    const fs_key key = fs_drop_key(drop, head);
     const int nblk = it.y;
     if (bucket_sums) {
         bucket_sums += ((int64_t)head * a.n_items + turn) * bias.n_buckets;
@@ -68,7 +74,7 @@ k_heads_rows(fs_walk a, fs_operand X, fs_operand Y, fs_operand H, fs_operand out
     const uint32_t y_colb = tile_y::column_bytes(lane, d), h_colb = tile_h::column_bytes(lane, N);
 
     BlockDesc d0 = block(0), d1 = block(1);
-    int cols0 = fs_block_cols(a, d0, lane), cols1 = fs_block_cols(a, d1, lane);
+    int cols0 = fs_first_cols(a, it, lane), cols1 = fs_block_cols(a, d1, lane);
     uint32_t bits0 = fs_row_bits<V>(a, it.x, 0, nblk, lane);
     // of the window: X's and g's rows, and lse (in units of log2) and D of row j
     fs_frag xf[KS], gf[KN], of[KN];
@@ -86,11 +92,6 @@ k_heads_rows(fs_walk a, fs_operand X, fs_operand Y, fs_operand H, fs_operand out
     tile_h h;
     y.load(Yb, Y.pitch, y_colb, cols0, lane);
     h.load(Hb, H.pitch, h_colb, cols0, lane);
-    if (bias.n_buckets > 0) {
-        fs_load_buckets(bias, lut, lane, 64);
-        for (int i = lane; i < bias.n_buckets; i += 64) table[i] = fs_flagless_log2(fs_widen<DT>(bias.table[head * bias.ld + i]));
-    }
-    const fs_key key = fs_drop_key(drop, head);
     const bool looks_up = bias.n_buckets > 0 || drop.state;
 
     fs_f4 acc[2 * KS];
@@ -111,7 +112,7 @@ k_heads_rows(fs_walk a, fs_operand X, fs_operand Y, fs_operand H, fs_operand out
         FS_WAVE_SYNC();
         int n_entries = 0;
         if (looks_up) {
-            n_entries = entries.make_list(bits0, lane);
+            n_entries = entries.make_list(bits0, lane, drop.state);
             entries.template look_up<false>(n_entries, lane, d0.w * V, cols0, lds_cols, bias, table, lut, drop, key);
         }
         h.put(lds, lane, N);
@@ -224,6 +225,17 @@ k_heads_cols(fs_walk a, int64_t rows, fs_operand X, fs_operand Y, fs_operand H, 
     const int turn = __builtin_amdgcn_readfirstlane(fs_launch_turn<1>(blockIdx.x, a.slice, a.n_swz));
     if (turn >= a.n_items) return;
     const int4 it = a.items[turn];
+    if (bias.n_buckets > 0) {
+        fs_load_buckets(bias, lut, lane, 64);
+        for (int i = lane; i < bias.n_buckets * share; i += 64)
+            table[i] = fs_flagless_log2(fs_widen<DT>(bias.table[(kv * share + i / bias.n_buckets) * bias.ld + i % bias.n_buckets]));
+    }
+    fs_key keys = fs_key{0u, 0u};  // lane i: that of the group's head i
+    if (drop.state) {
+        const uint64_t seed = (uint64_t)drop.state[0], at = (uint64_t)drop.state[1];
+        keys = fs_threefry<20>(fs_key{(uint32_t)seed, (uint32_t)(seed >> 32)}, (uint32_t)at, (uint32_t)(at >> 32));
+        keys = fs_threefry<20>(keys, (uint32_t)(kv * share + lane), 0u);
+    }
     const int nblk = it.y;
     if (nblk == 0) return;
     int slot = it.z;
@@ -243,24 +255,12 @@ k_heads_cols(fs_walk a, int64_t rows, fs_operand X, fs_operand Y, fs_operand H, 
         st = row_stats[head * rows + row_of_lane];
     };
     BlockDesc d0 = block(0), d1 = block(1);
-    int rows0 = fs_block_cols(a, d0, lane), rows1 = fs_block_cols(a, d1, lane);
+    int rows0 = fs_first_cols(a, it, lane), rows1 = fs_block_cols(a, d1, lane);
     uint32_t bits0 = fs_row_bits<V>(a, it.x, 0, nblk, lane), bits1 = fs_row_bits<V>(a, it.x, 1, nblk, lane);
     fs_frag yf[KS], hf[KN];
     fs_load_window<V>(yf, Yb, Y.pitch, d, d0.w, a.M, lane);
     fs_load_window<V>(hf, Hb, H.pitch, N, d0.w, a.M, lane);
     gather(0, rows0);
-    if (bias.n_buckets > 0) {
-        fs_load_buckets(bias, lut, lane, 64);
-        for (int i = lane; i < bias.n_buckets * share; i += 64)
-            table[i] = fs_flagless_log2(fs_widen<DT>(bias.table[(kv * share + i / bias.n_buckets) * bias.ld + i % bias.n_buckets]));
-    }
-    fs_key keys = fs_key{0u, 0u};  // lane i: that of the group's head i
-    if (drop.state) {
-        const uint64_t seed = (uint64_t)drop.state[0], at = (uint64_t)drop.state[1];
-        keys = fs_threefry<20>(fs_key{(uint32_t)seed, (uint32_t)(seed >> 32)}, (uint32_t)at, (uint32_t)(at >> 32));
-        keys = fs_threefry<20>(keys, (uint32_t)(kv * share + lane), 0u);
-    }
-
     fs_f4 acc_y[2 * KS], acc_h[NT];
     fs_clear(acc_y);
     fs_clear(acc_h);
@@ -287,7 +287,7 @@ k_heads_cols(fs_walk a, int64_t rows, fs_operand X, fs_operand Y, fs_operand H, 
         FS_WAVE_SYNC();
         if (looks_up) {
             const fs_key key = fs_key{(uint32_t)__builtin_amdgcn_readlane((int)keys.k0, member), (uint32_t)__builtin_amdgcn_readlane((int)keys.k1, member)};
-            if (member == 0) n_entries = entries.make_list(bits0, lane);
+            if (member == 0) n_entries = entries.make_list(bits0, lane, drop.state);
             entries.template look_up<true>(n_entries, lane, d0.w * V, rows0, lds_rows, bias, table + member * bias.n_buckets, lut, drop, key);
         }
         fs_f4 sc[2], gp[2];
