@@ -413,14 +413,15 @@ fs_status fs_edge_dropout(const fs_format *fmt, int32_t heads, const void *d_in_
  *   s = scale * (X_h * Y_g^T) + bias_h at the stored positions of A,  P = softmax_rows(s),
  *   out_h = dropout(P) * H_g,   lse_h = log of the row sums of exp(s).
  *   X : M x d, out : M x N for each of `heads`;  Y : K x d, H : K x N for each of kv_heads, which divides heads
- *   d % 8 == 0, N % 8 == 0, both at most 128; leading dimensions and head strides % 8 == 0, pointers 16-byte aligned
+ *   d % 8 == 0, N % 8 == 0, both at most 128; leading dimensions and head strides % 8 == 0, pointers 16-byte aligned;
+ *           at most 65535 heads, 64 of them for one of kv_heads
  *   bias, drop : NULL for none (the pass of serving is this call without dropout)
  *   d_lse : heads x M floats, 4-byte aligned, or NULL; a row without entries gets zeros and minus infinity
  *   d_work : fs_attention_forward_workspace_bytes, 16-byte aligned (may be NULL when that size is 0)
- * Scores and probabilities stay in registers in fp32; probabilities are rounded to the element type relative to the running row
+ * out and d_lse overlap nothing that is read.  Scores and probabilities stay in registers in fp32; probabilities are rounded to the element type relative to the running row
  * maximum for the product with H.  M and K below 2^24; a head of X, Y and H spans less than 4 GiB, a row pitch is below
- * 2^24 bytes (else FS_ERR_UNSUPPORTED).  As in fs_spmm, inputs are taken to be finite: an infinity or NaN in a row of H reaches all
- * rows of the windows that reference it.  Asynchronous on `stream`; deterministic.
+ * 2^24 bytes (else FS_ERR_UNSUPPORTED).  As in fs_spmm, an infinity or NaN in a row of H reaches all
+ * rows of the windows that reference it; one in a row of X or Y reaches the scores of the entries it has, not their neighbours'.  Asynchronous on `stream`; deterministic.
  */
 fs_status fs_attention_forward_workspace_bytes(const fs_format *fmt, int32_t heads, int64_t N, size_t *work_bytes);
 fs_status fs_attention_forward(const fs_format *fmt, int32_t heads, int32_t kv_heads, int64_t d, int64_t N, float scale,
@@ -434,7 +435,8 @@ fs_status fs_attention_forward(const fs_format *fmt, int32_t heads, int32_t kv_h
  *   dX = scale * dS * Y,  dY = scale * dS^T * X,  dH = (Z * P)^T * G,  dtable[h][k] = sum of dS over bucket k,
  * dY and dH summed over the query heads that share them.  Two passes: by rows over fmt (dX, dtable) and by columns over
  * fmt_t, the format of A^T (fs_csr_transpose, fs_convert).  Scores are computed again from X and Y; dS and Z * P are rounded
- * to the element type for the products (fp16: loss scaling keeps dS out of its subnormal range).
+ * to the element type for the products (fp16: loss scaling keeps dS out of its subnormal range).  An infinity or NaN in a row of Y,
+ * X or G reaches the gradients of all rows of the windows that reference it.
  *   X, Y, H, bias, drop, scale : as in the forward call, whose out and lse these are;  G : M x N for each of `heads`
  *   dX, dY, dH : written whole (zeros where nothing is stored), and overlap nothing that is read
  *   d_table_grad : heads * n_buckets elements in the element type, 2-byte aligned, or NULL

@@ -275,9 +275,14 @@ __device__ __forceinline__ int fs_block_cols(const fs_walk &a, const BlockDesc &
     return a.vec_col[max(min(b.s + min(lane & 31, b.kb - 1), a.nvec - 1), 0)];
 }
 
-// The same for the first block of an item, whose first vector stands in the item's record: beside its descriptor, not after it.  Vectors
-// past its width are the next block's, whose products nobody reads.
+// The same for the first block of an item, whose first vector stands in the item's record: the load is issued beside the descriptor's, not
+// after it (fs_first_cols), and cut to the block's width when that is known.
 __device__ __forceinline__ int fs_first_cols(const fs_walk &a, const int4 &item, int lane) { return a.vec_col[min(item.w + (lane & 31), a.nvec - 1)]; }
+__device__ __forceinline__ int fs_cut_cols(int cols, int kb, int lane)
+{
+    const int last = __builtin_amdgcn_readlane(cols, max(kb - 1, 0));
+    return (lane & 31) < kb ? cols : last;
+}
 
 // Occupancy of window row j in block i of an item: bit c, the row stores the block's vector c (none for lanes past V).
 template <int V>

@@ -55,8 +55,10 @@ k_heads_forward(fs_walk a, fs_operand X, fs_operand Y, fs_operand H, int share, 
     const unsigned char *Xb = X.p + head * X.head, *Yb = Y.p + head / share * Y.head, *Hb = H.p + head / share * H.head;
     const uint32_t y_colb = tile_y::column_bytes(lane, d), h_colb = tile_h::column_bytes(lane, N);
 
+    int cols0 = fs_first_cols(a, it, lane);
     BlockDesc d0 = block(0), d1 = block(1);
-    int cols0 = fs_first_cols(a, it, lane), cols1 = fs_block_cols(a, d1, lane);
+    cols0 = fs_cut_cols(cols0, d0.kb, lane);
+    int cols1 = fs_block_cols(a, d1, lane);
     uint32_t bits0 = fs_row_bits<V>(a, it.x, 0, nblk, lane);
     fs_frag xf[KS];
     fs_load_window<V>(xf, Xb, X.pitch, d, d0.w, a.M, lane);

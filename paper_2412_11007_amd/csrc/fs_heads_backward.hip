@@ -73,8 +73,10 @@ k_heads_rows(fs_walk a, fs_operand X, fs_operand Y, fs_operand H, fs_operand out
     const unsigned char *Gb = G.p + head * G.head, *Ob = out.p + head * out.head;
     const uint32_t y_colb = tile_y::column_bytes(lane, d), h_colb = tile_h::column_bytes(lane, N);
 
+    int cols0 = fs_first_cols(a, it, lane);
     BlockDesc d0 = block(0), d1 = block(1);
-    int cols0 = fs_first_cols(a, it, lane), cols1 = fs_block_cols(a, d1, lane);
+    cols0 = fs_cut_cols(cols0, d0.kb, lane);
+    int cols1 = fs_block_cols(a, d1, lane);
     uint32_t bits0 = fs_row_bits<V>(a, it.x, 0, nblk, lane);
     // of the window: X's and g's rows, and lse (in units of log2) and D of row j
     fs_frag xf[KS], gf[KN], of[KN];
@@ -254,8 +256,10 @@ k_heads_cols(fs_walk a, int64_t rows, fs_operand X, fs_operand Y, fs_operand H, 
         g_.load(G.p + head * G.head, G.pitch, g_colb, row_of_lane, lane);
         st = row_stats[head * rows + row_of_lane];
     };
+    int rows0 = fs_first_cols(a, it, lane);
     BlockDesc d0 = block(0), d1 = block(1);
-    int rows0 = fs_first_cols(a, it, lane), rows1 = fs_block_cols(a, d1, lane);
+    rows0 = fs_cut_cols(rows0, d0.kb, lane);
+    int rows1 = fs_block_cols(a, d1, lane);
     uint32_t bits0 = fs_row_bits<V>(a, it.x, 0, nblk, lane), bits1 = fs_row_bits<V>(a, it.x, 1, nblk, lane);
     fs_frag yf[KS], hf[KN];
     fs_load_window<V>(yf, Yb, Y.pitch, d, d0.w, a.M, lane);

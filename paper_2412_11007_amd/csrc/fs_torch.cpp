@@ -226,12 +226,12 @@ struct Heads {
     void set(const at::Tensor &t, const fs_format *f, int64_t rows)
     {
         const int64_t dim = t.dim();
-        if ((dim != 2 && dim != 3) || !of_format(t, f) || t.size(0) != rows || t.stride(dim - 1) != 1) return;
+        if ((dim != 2 && dim != 3) || !of_format(t, f) || t.size(0) != rows || (t.stride(dim - 1) != 1 && rows > 0)) return;
         heads = dim == 3 ? t.size(1) : 1;
         columns = t.size(dim - 1);
         m.d = t.data_ptr();
-        m.ld = rows > 1 ? t.stride(0) : std::max(t.stride(0), columns);
-        m.head = heads > 1 ? t.stride(1) : dim == 2 ? 0 : columns;
+        m.ld = rows == 0 ? heads * columns : rows > 1 ? t.stride(0) : std::max(t.stride(0), columns);  // (nothing is read by a stride that nothing needs)
+        m.head = dim == 2 ? 0 : rows == 0 || heads == 1 ? columns : t.stride(1);
         ok = true;
     }
 };

@@ -265,6 +265,68 @@ def test_results_repeat_bit_for_bit_on_another_stream_and_in_a_graph(fs):
 
 
 
+@pytest.mark.parametrize("V", [4, 8, 16])
+@pytest.mark.parametrize("p,bias", [(0.3, None), (0.0, (5, 9)), (0.3, (5, 9))])
+def test_infinities_and_nan_in_rows_nobody_stores(fs, V, p, bias):
+    """Rows of Y and H (backward: of X and the gradient) that a window does not reference hold no finite number, the next block's vectors
+    in the arrays among them: nothing of them arrives."""
+    import torch
+    a = Problem(fs, 16, 64, 90, 2, 1, 32, 48, "bf16", kind="band", p=p, bias=bias, V=V, V_t=V)
+    out, lse, grads = a.check()
+    bad = ~a.stored.any(0)
+    assert bad.any()
+    rows = torch.from_numpy(np.nonzero(bad)[0]).cuda()
+    a.Y[rows], a.H[rows] = float("nan"), float("inf")
+    got = a.forward()
+    assert torch.equal(got[0], out) and torch.equal(got[1], lse)
+    assert all(torch.equal(x, y) for x, y in zip(a.backward(out, lse), grads) if y is not None)
+    # a row that only the last window references
+    b = Problem(fs, 17, 64, 64, 1, 1, 32, 48, "f16", kind="random", p=p, bias=bias, V=V, V_t=V)
+    stored = b.stored.copy()
+    stored[:, 5] = False
+    stored[-1, 5] = True
+    rp, ci = csr_of(stored)
+    b.fmt = fs.fs_convert(rp, ci, None, 64, 64, torch_dtype=torch.float16, V=V)
+    want = b.forward()[0].clone()
+    b.H[5] = float("inf")
+    b.Y[5] = float("nan")
+    got = b.forward()[0]
+    last = (64 - 1) // V * V
+    assert torch.equal(got[:last], want[:last]) and torch.isnan(got[-1]).all()
+
+
+@pytest.mark.parametrize("M,K", [(0, 5), (5, 0), (0, 0)])
+def test_no_rows_or_no_columns(fs, M, K):
+    a = Problem(fs, 18, M, K, 2, 1, 16, 16, "f16", kind="empty", p=0.2, bias=(4, 3))
+    out, lse = a.forward()
+    assert out.shape == (M, 2, 16) and not out.any() and (lse == -np.inf).all()
+    assert not any(g.any() for g in a.backward(out, lse))
+
+
+def test_the_most_heads_for_one_of_keys_the_most_buckets_and_widths(fs):
+    """64 query heads that share keys and values, 128 buckets, 1024 positions either way, 128 columns: the most LDS a call takes."""
+    for V in (4, 16):
+        Problem(fs, 19, 33, 40, 64, 1, 128, 128, "bf16", kind="random", p=0.2, bias=(128, 1024), V=V, V_t=V).check()
+
+
+def test_two_calls_at_once_on_two_streams(fs):
+    """Calls own what they write: two in flight give what they give alone."""
+    import torch
+    a = Problem(fs, 20, 700, 600, 2, 2, 64, 64, "f16", kind="hub", p=0.2, bias=(32, 100), chunk=64)
+    b = Problem(fs, 21, 500, 800, 4, 1, 32, 32, "bf16", kind="hub", p=0.4, bias=(16, 50), chunk=64)
+    want = [x.forward() + x.backward(*x.forward()) for x in (a, b)]
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    for _ in range(3):
+        got = [[], []]
+        for i, x in enumerate((a, b)):
+            with torch.cuda.stream(streams[i]):
+                o, l = x.forward()
+                got[i] = (o, l) + x.backward(o, l)
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for g, w in zip(got, want) for x, y in zip(g, w))
+
+
 @pytest.mark.parametrize("dtype", ["f16", "bf16"])
 @pytest.mark.parametrize("V", [4, 8, 16])
 @pytest.mark.parametrize("heads", [1, 3])
