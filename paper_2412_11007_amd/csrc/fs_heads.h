@@ -57,6 +57,23 @@ __device__ __forceinline__ int fs_lane_here(int lane)
     return lane;
 }
 
+// Reductions over the four lanes of a row, l, l ^ 16, l ^ 32 and l ^ 48: rows of sixteen lanes, then halves of the wavefront, change places in
+// two copies of a register (no LDS traffic, no address).
+__device__ __forceinline__ float fs_row_max(float v)
+{
+    auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1]));
+    p = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1]));
+}
+__device__ __forceinline__ float fs_row_sum(float v)
+{
+    auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = __uint_as_float(p[0]) + __uint_as_float(p[1]);
+    p = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(p[0]) + __uint_as_float(p[1]);
+}
+
 // What the kernels are given of a bias and of a dropout (n_buckets = 0, state null: none).
 struct fs_bias_args {
     const uint16_t *table;
@@ -324,9 +341,10 @@ struct fs_entries {
     }
     // T: window rows are columns of A.  cols: lane l holds the column (T: row) of vector l mod 32; lds_cols the same in LDS.
     template <bool T>
-    __device__ __forceinline__ void look_up(int n, int lane, int row0, int cols, const int *lds_cols, const fs_bias_args &b, const float *table,
+    __device__ __forceinline__ void look_up(int n, int lane_, int row0, int cols, const int *lds_cols, const fs_bias_args &b, const float *table,
                                             const uint8_t *lut, const fs_drop_args &drop, fs_key key)
     {
+        const int lane = fs_lane_here(lane_);
         auto bucket = [&](int j, int col) -> int { return fs_bucket_of(lut, b.reach, b.shift, T ? col : row0 + j, T ? row0 + j : col); };
         auto keep = [&](int j, int col) -> uint32_t {
             return fs_threefry<13>(key, (uint32_t)(T ? col : row0 + j), (uint32_t)(T ? row0 + j : col)).k0 >= drop.below ? 1u : 0u;
@@ -379,8 +397,9 @@ struct fs_entries {
         FS_WAVE_SYNC();
     }
     // of the lane's places: row j, vectors 8g .. 8g+7
-    __device__ __forceinline__ void values(float (&v)[8], int lane) const
+    __device__ __forceinline__ void values(float (&v)[8], int lane_) const
     {
+        const int lane = fs_lane_here(lane_);
         const fs_f4 *from = reinterpret_cast<const fs_f4 *>(value + (lane & (V - 1)) * kPitch + 8 * (lane >> 4));
         const fs_f4 lo = from[0], hi = from[1];
 #pragma unroll
@@ -389,8 +408,9 @@ struct fs_entries {
             v[4 + x] = hi[x];
         }
     }
-    __device__ __forceinline__ void put_values(const float (&v)[8], int lane)
+    __device__ __forceinline__ void put_values(const float (&v)[8], int lane_)
     {
+        const int lane = fs_lane_here(lane_);
         if ((lane & 15) >= V) return;
         fs_f4 *to = reinterpret_cast<fs_f4 *>(value + (lane & 15) * kPitch + 8 * (lane >> 4));
         to[0] = fs_f4{v[0], v[1], v[2], v[3]};

@@ -23,7 +23,7 @@
 namespace {
 
 template <int DT, int V, int KS, int NT>
-__global__ void __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(KS <= 2 && NT <= 4 ? 4 : KS > 1 && NT == 8 ? 2 : 3)))
+__global__ void __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(KS <= 2 && NT <= 4 ? 4 : KS * NT <= 16 ? 3 : 2)))
 k_heads_forward(fs_walk a, fs_operand X, fs_operand Y, fs_operand H, int share, int d, int N, float sl2, fs_bias_args bias, fs_drop_args drop,
                 fs_operand out, float *__restrict__ lse, float *__restrict__ part, float *__restrict__ stats)
 {
@@ -76,7 +76,7 @@ k_heads_forward(fs_walk a, fs_operand X, fs_operand Y, fs_operand H, int share, 
     int step = 0;
     auto block_step = [&](auto more_) {
         constexpr bool MORE = decltype(more_)::value;
-        if (lane < 32) lds_cols[lane] = cols0;
+        if (const int l = fs_lane_here(lane); l < 32) lds_cols[l] = cols0;
         const BlockDesc d2 = block(step + 2);
         int cols2 = 0;
         uint32_t bits1 = 0;
@@ -119,9 +119,7 @@ k_heads_forward(fs_walk a, fs_operand X, fs_operand Y, fs_operand H, int share, 
             p[x] = fs_choose(fs_bit_mask(m8, x), p[x], -INFINITY);
             mx = fmaxf(mx, p[x]);
         }
-        mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
-        mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-        const float m_new = fmaxf(m_run, mx);
+        const float m_new = fmaxf(m_run, fs_row_max(mx));
         const float m_use = m_new == -INFINITY ? 0.f : m_new;  // nothing seen so far
         const float corr = __builtin_amdgcn_exp2f(m_run - m_use);
         float ps = 0.f;
@@ -144,8 +142,7 @@ k_heads_forward(fs_walk a, fs_operand X, fs_operand Y, fs_operand H, int share, 
         }
         FS_WAVE_SYNC();
         if (d0.last || !MORE) {
-            float l_tot = l_run + __shfl_xor(l_run, 16, 64);
-            l_tot += __shfl_xor(l_tot, 32, 64);
+            const float l_tot = fs_row_sum(l_run);
             const int l = fs_lane_here(lane), j = l & 15, g = l >> 4, row = d0.w * V + j;
             if (d0.last && from_first) {
                 fs_store_window<DT, V, 16 * NT>(lds, acc, l_tot == 0.f ? 0.f : drop.factor / l_tot, out.p + head * out.head, out.pitch, N, d0.w, a.M, lane);

@@ -25,11 +25,11 @@
 
 namespace {
 
-constexpr int kSumColumns = 32;  // of the table of sums in LDS, for each bucket
+constexpr int kSumColumns = 16;  // of the table of sums in LDS, for each bucket
 __host__ __device__ constexpr float fs_weight_scale(int dtype) { return dtype == FS_F16 ? 4096.f : 1.f; }  // of Z P
 
 template <int DT, int V, int KS, int NT>
-__global__ void __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(KS * NT <= 4 ? 4 : KS <= 2 && NT <= 4 ? 3 : 2)))
+__global__ void __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(KS <= 2 && NT <= 4 ? 4 : KS * NT <= 8 ? 3 : 2)))
 k_heads_rows(fs_walk a, fs_operand X, fs_operand Y, fs_operand H, fs_operand out, fs_operand G, const float *__restrict__ lse, int share, int d, int N,
              float sl2, float scale, fs_bias_args bias, fs_drop_args drop, fs_operand dX, float2 *__restrict__ row_stats, float *__restrict__ part,
              float *__restrict__ bucket_sums)
@@ -84,12 +84,15 @@ k_heads_rows(fs_walk a, fs_operand X, fs_operand Y, fs_operand H, fs_operand out
     auto load_window = [&](int w) {
         fs_load_window<V>(xf, Xb, X.pitch, d, w, a.M, lane);
         fs_load_window<V>(gf, Gb, G.pitch, N, w, a.M, lane);
+    };
+    auto load_stats = [&](int w) {
         fs_load_window<V>(of, Ob, out.pitch, N, w, a.M, lane);
         const int j = fs_lane_here(lane) & 15;
         const int64_t row = (int64_t)w * V + j;
         if (j < V && row < a.M) my_lse = lse[(int64_t)head * a.M + row];
     };
     load_window(d0.w);
+    load_stats(d0.w);
     tile_y y;
     tile_h h;
     y.load(Yb, Y.pitch, y_colb, cols0, lane);
@@ -103,7 +106,7 @@ k_heads_rows(fs_walk a, fs_operand X, fs_operand Y, fs_operand H, fs_operand out
     int step = 0;
     auto block_step = [&](auto more_) {
         constexpr bool MORE = decltype(more_)::value;
-        if (lane < 32) lds_cols[lane] = cols0;
+        if (const int l = fs_lane_here(lane); l < 32) lds_cols[l] = cols0;
         const BlockDesc d2 = block(step + 2);
         int cols2 = 0;
         uint32_t bits1 = 0;
@@ -119,19 +122,6 @@ k_heads_rows(fs_walk a, fs_operand X, fs_operand Y, fs_operand H, fs_operand out
         }
         h.put(lds, lane, N);
         if constexpr (MORE) h.load(Hb, H.pitch, h_colb, cols1, lane);
-        if (new_window) {
-            const int j = fs_lane_here(lane) & 15, row = d0.w * V + j;
-            D = 0.f;
-#pragma unroll
-            for (int ks = 0; ks < KN; ks++)
-#pragma unroll
-                for (int k = 0; k < 8; k++) D = fmaf(fs_widen<DT>(gf[ks].e[k]), fs_widen<DT>(of[ks].e[k]), D);
-            D += __shfl_xor(D, 16, 64);
-            D += __shfl_xor(D, 32, 64);
-            // a row of which nothing is left: exp(s - lse) has to come out as zero
-            lse2 = my_lse == -INFINITY ? INFINITY : my_lse * 1.44269504088896340736f;
-            if (d0.first && g == 0 && j < V && row < a.M) row_stats[(int64_t)head * a.M + row] = make_float2(lse2, D);
-        }
         FS_WAVE_SYNC();
         fs_f4 sc[2], gp[2];
 #pragma unroll
@@ -142,6 +132,18 @@ k_heads_rows(fs_walk a, fs_operand X, fs_operand Y, fs_operand H, fs_operand out
         FS_WAVE_SYNC();
 #pragma unroll
         for (int t = 0; t < 2; t++) sc[t] = tile_y::template contract<DT>(lds, t, lane, xf);
+        if (new_window) {
+            const int j = fs_lane_here(lane) & 15, row = d0.w * V + j;
+            D = 0.f;
+#pragma unroll
+            for (int ks = 0; ks < KN; ks++)
+#pragma unroll
+                for (int k = 0; k < 8; k++) D = fmaf(fs_widen<DT>(gf[ks].e[k]), fs_widen<DT>(of[ks].e[k]), D);
+            D = fs_row_sum(D);
+            // a row of which nothing is left: exp(s - lse) has to come out as zero
+            lse2 = my_lse == -INFINITY ? INFINITY : my_lse * 1.44269504088896340736f;
+            if (d0.first && g == 0 && j < V && row < a.M) row_stats[(int64_t)head * a.M + row] = make_float2(lse2, D);
+        }
         new_window = MORE && d1.w != d0.w;
         if (new_window) load_window(d1.w);
         const uint32_t m8 = bits0 >> (8 * g);
@@ -164,7 +166,7 @@ k_heads_rows(fs_walk a, fs_operand X, fs_operand Y, fs_operand H, fs_operand out
             FS_WAVE_SYNC();
             entries.put_values(ds, lane);
             FS_WAVE_SYNC();
-            for (int r = lane; r < n_entries; r += 64) {
+            for (int r = fs_lane_here(lane); r < n_entries; r += 64) {
                 const int code = entries.list[r];
                 const float v = entries.value[(code >> 5 & 15) * entries.kPitch + (code & 31)];
                 float *cell = sums + COLS * (code >> 9) + (lane & (COLS - 1));
@@ -179,6 +181,7 @@ k_heads_rows(fs_walk a, fs_operand X, fs_operand Y, fs_operand H, fs_operand out
             for (int t = 0; t < 2 * KS; t++) acc[t] = fs_mfma_16x16x32<DT>(tile_y::transposed(lds, t, lane), sp, acc[t]);
         }
         FS_WAVE_SYNC();
+        if (new_window) load_stats(d1.w);
         if (d0.last || !MORE) {
             if (d0.last && from_first) {
                 fs_store_window<DT, V, 32 * KS>(lds, acc, scale, dX.p + head * dX.head, dX.pitch, d, d0.w, a.M, lane);
@@ -275,9 +278,9 @@ k_heads_cols(fs_walk a, int64_t rows, fs_operand X, fs_operand Y, fs_operand H, 
         const bool block_done = member + 1 == share, done = block_done && step + 1 == nblk;
         x_.put(lds_x, lane, d);
         g_.put(lds_g, lane, N);
-        if (lane < 32) {
-            lds_rows[lane] = rows0;
-            lds_stats[lane] = st;
+        if (const int l = fs_lane_here(lane); l < 32) {
+            lds_rows[l] = rows0;
+            lds_stats[l] = st;
         }
         BlockDesc d2 = d1;
         int rows2 = rows1;
