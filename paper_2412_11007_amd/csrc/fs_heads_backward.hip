@@ -166,13 +166,17 @@ k_heads_rows(fs_walk a, fs_operand X, fs_operand Y, fs_operand H, fs_operand out
             FS_WAVE_SYNC();
             entries.put_values(ds, lane);
             FS_WAVE_SYNC();
-            for (int r = fs_lane_here(lane); r < n_entries; r += 64) {
-                const int code = entries.list[r];
+            const int l = fs_lane_here(lane);
+            for (int r0 = 0; r0 < n_entries; r0 += 64) {
+                const bool mine = r0 + l < n_entries;
+                const int code = mine ? entries.list[r0 + l] : 0;
                 const float v = entries.value[(code >> 5 & 15) * entries.kPitch + (code & 31)];
-                float *cell = sums + COLS * (code >> 9) + (lane & (COLS - 1));
+                float *cell = sums + COLS * (code >> 9) + (l & (COLS - 1));
 #pragma unroll
-                for (int turn_ = 0; turn_ < 64 / COLS; turn_++)  // no two lanes of a turn share a cell
-                    if (lane / COLS == turn_) *cell += v;
+                for (int turn_ = 0; turn_ < 64 / COLS; turn_++) {  // no two lanes of a turn share a cell; the fence keeps the turns apart,
+                    if (mine && l / COLS == turn_) *cell += v;     // which look like one to a compiler that sees a lane at a time
+                    FS_WAVE_SYNC();
+                }
             }
         }
         const fs_frag sp = fs_round8<DT>(ds);
