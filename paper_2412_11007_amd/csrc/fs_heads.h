@@ -167,10 +167,6 @@ inline fs_drop_args fs_drop_of(const fs_dropout *d)
     return fs_drop_args{d->d_state, (uint32_t)(d->p * 4294967296.0), (float)(1.0 / (1.0 - d->p))};
 }
 
-// Wavefronts for one head's gradient of a bias table on a value array: enough to fill the chip (a table of 32 buckets takes
-// 8 KB of LDS, twenty of them a CU), few enough that their tables are soon added.
-inline int fs_edge_gradient_waves(int heads) { return std::max(256, 4096 / std::max(heads, 1)); }
-
 // Sums over `n` tables go through this many partial ones (0: straight).
 constexpr int kBucketSumGroups = 64;
 inline size_t fs_bucket_sums_floats(int64_t heads, int64_t n, int64_t n_buckets) { return (size_t)heads * (size_t)(n + kBucketSumGroups) * (size_t)n_buckets; }
