@@ -277,7 +277,7 @@ fs_status fs_bucket_sums_launch(int dtype, int heads, int n, int n_buckets, floa
 {
     int log2_buckets = 0;
     while (1 << log2_buckets < n_buckets) log2_buckets++;
-    if (n > 1024) {
+    if (((int64_t)n << log2_buckets) > 64 * 1024) {  // one workgroup a head adds 64 sums a thread in 4 us; two launches take 6 and 2.5 us more of the host
         float *part = sums + (size_t)heads * n * n_buckets;
         k_bucket_sums<-1><<<dim3(kBucketSumGroups, heads), 1024, 0, st>>>(sums, n, n_buckets, log2_buckets, part);
         FS_LAUNCH_CHECK();
