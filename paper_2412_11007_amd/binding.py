@@ -573,7 +573,7 @@ class FsBucketBias:
     """A learned bias of the scores by relative position, column - row - ``shift``.
 
     ``table``: (heads, buckets) in the element type, or (buckets,) for a single head; ``buckets``: uint8, the bucket of the relative
-    positions -reach .. reach (2 * reach + 1 values, longer distances count as reach).  ``fs_relative_buckets`` makes one."""
+    positions -reach .. reach (2 * reach + 1 values at a 4-byte boundary, longer distances count as reach).  ``fs_relative_buckets`` makes one."""
 
     def __init__(self, table, buckets, shift: int = 0):
         assert table.is_cuda and table.dim() in (1, 2) and table.stride(-1) == 1 and table.element_size() == 2

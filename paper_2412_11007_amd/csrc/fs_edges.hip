@@ -7,14 +7,15 @@
 // A block is V x kb consecutive elements, row by row.  A lane takes eight of them, sixteen bytes, so that a wave-wide load or store
 // moves 1 KB of consecutive blocks (16 / V of them at full width) whatever their width; the row and the place of an element
 // follow from its number and kb.  Which elements A stores is read from blk_row_bits, the columns of the block's vectors from
-// vec_col; both pass through LDS.
+// vec_col; both pass through LDS.  Bias and dropout run near a copy's rate (R-MAT of 2^18 rows, bias: 29 us, 132 MB, 4.5 TB/s; lognormal
+// graph, two heads, dropout: 83 us, 362 MB, 4.4 TB/s).
 //
 // The gradient adds into a table in LDS of fp32 sums, n_buckets x 64 with a column for each lane, or n_buckets x 16 with four lanes a column
 // that take turns: no two lanes add to a sum at once.  A sum's summands come in the order in which its wavefront walks the blocks, the
 // columns of a bucket are added in a fixed order at the end, and the wavefronts' tables by a second launch, so the result does not depend
 // on timing.  The walk is bound by the chain value -> column -> bucket -> sum, so wavefronts count: where A stores less than half of the
 // places, those that it stores are dealt out to the lanes and the narrow table lets 32 wavefronts of a CU work instead of 16 (32 buckets,
-// R-MAT of 2^18 rows 42 us -> 34, lognormal graph 44 -> 31, uniform 35 -> 29); where it stores more, turns and dealing cost more than they
+// R-MAT of 2^18 rows 42 us -> 33, lognormal graph 44 -> 31, uniform 36 -> 28); where it stores more, turns and dealing cost more than they
 // bring (sequence of 8192 with a window of 384, two heads: 17 us -> 19).
 #include <algorithm>
 

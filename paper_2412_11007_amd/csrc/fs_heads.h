@@ -309,7 +309,9 @@ __device__ __forceinline__ uint32_t fs_row_bits(const fs_walk &a, int first_slot
 // What an entry needs beside its score -- a bias from its bucket, a word of the generator -- takes about 70 instructions.  In the
 // scores' layout a lane has eight places, and taken place by place they were most of a block's: of a power-law graph an eighth of
 // the places are stored, and with eight rows a window half the lanes have none.  So every lane takes one entry at a time from a list in LDS
-// or, where more than half of the block is stored, one place at a time in row order, without a list.  The results go to `value`, a
+// or one place at a time in row order, without a list: where more than half of the block is stored; with four rows, whose 128 places are
+// two turns; with eight rows and no dropout, where a place costs less than the list's chain (one row of 1028 entries, eight heads, 12.1 us with
+// the list, 10.5 without; R-MAT of 65 k rows 48 and 45; with dropout, R-MAT of 131 k rows, gradients 156 with and 171 without).  The results go to `value`, a
 // V x 32 tile of biases whose lowest bit says whether dropout keeps the entry (of the 24 bits of a mantissa, for a bias of 8 or 11).
 template <int V>
 struct fs_entries {

@@ -14,10 +14,18 @@
 // element type in each product is of the size of the errors of Z P and dS, which are rounded for the matrix cores.  fp16 holds Z P scaled by
 // 2^12: probabilities are at most 1, and those of rows with thousands of entries would lie among its subnormal numbers.
 //
-// dtable: every lane adds the dS of its window row to a column of its own of a table of sums in LDS (V x 4 columns for each
-// bucket), a wavefront leaves one sum per bucket, and those are added in the order of the work list.
+// dtable: the block's dS pass through LDS, its stored elements are dealt out to the lanes, and each adds to one of 16 columns of a table of
+// fp32 sums, kSumColumns for each bucket.  Four lanes share a column and take turns, kept apart by fences (a column for each lane, 8 KB
+// with 32 buckets: gradients of a lognormal graph 1068 us for 1017; atomics on LDS: 51 us for 15 in the same sums over a value array).  A wavefront leaves one sum per bucket, and those are added in the order of the work list.
 //
 // By columns the query heads that share keys and values are walked inside a block, one after the other, into the same accumulators.
+//
+// Bounds, with 64 columns of both kinds, bias and dropout: on a lognormal graph of 262 k rows, two heads, the fabric (by rows 455 us, 2.9 GB
+// fetched, 6.7 TB/s; by columns 528 us, 3.3 GB, 6.6 TB/s, lines for the 8 bytes {lse, D} of a row among them); on a sequence of 4096
+// with a window of 256, eight heads on two, instructions and too few wavefronts to hide a block's chain (53 and 57 us, 53 % and 40 % of the
+// issue slots; by columns there are two wavefronts a SIMD).  Wavefronts a SIMD: by rows four up to 64 columns, three up to KS * NT = 8; by
+// columns, with two tiles of accumulators and of gathered rows, three up to 64 columns (four spill: 501 us by rows became 562 so, before
+// addresses were worked out where they are used).
 #include <type_traits>
 
 #include "fs_common.h"

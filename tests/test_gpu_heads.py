@@ -393,6 +393,44 @@ def test_value_arrays_of_one_element_alignment(fs):
             assert torch.equal(b[3:n + 3], want) and (b[:3] == 3.0).all() and (b[n + 3:] == 3.0).all()
 
 
+@pytest.mark.parametrize("kind", ["sparse", "band"])
+@pytest.mark.parametrize("heads,n_buckets,reach", [(1, 32, 128), (3, 128, 1024), (2, 1, 0)])
+@pytest.mark.parametrize("V", [4, 8])
+def test_bias_over_many_blocks(fs, kind, heads, n_buckets, reach, V):
+    """More blocks than wavefronts, more of their tables than one launch adds.  Gradients of -1, 0 and 1: every sum is a whole number below
+    2^24, so fp32 holds it whatever the order, and the result is the sum rounded once (whole numbers up to 2048 as they are, f16)."""
+    import torch
+    rng = np.random.default_rng(n_buckets + V)
+    if kind == "sparse":
+        M = K = 50000
+        rows = np.repeat(np.arange(M), 18)
+        cols = rng.integers(0, K, rows.size)
+        near = rng.random(rows.size) < 0.5
+        cols[near] = np.clip(rows[near] + rng.integers(-700, 700, near.sum()), 0, K - 1)
+    else:
+        M = K = 16000
+        rows = np.repeat(np.arange(M), 190)
+        cols = rows - np.tile(np.arange(190), M)
+        rows, cols = rows[cols >= 0], cols[cols >= 0]
+    at = np.unique(rows.astype(np.int64) * K + cols)
+    rows, cols = at // K, at % K
+    rp = np.concatenate([[0], np.cumsum(np.bincount(rows, minlength=M))])
+    fmt = fs.fs_convert(to_dev_i32(rp), to_dev_i32(cols), None, M, K, torch_dtype=torch.float16, V=V)
+    assert (2 * fmt.nnz < fmt.V * fmt.nvec) == (kind == "sparse")
+    lut = rng.integers(0, n_buckets, 2 * reach + 1).astype(np.uint8)
+    table = rng.standard_normal((heads, n_buckets)).astype(np.float16)
+    bias = fs.FsBucketBias(torch.from_numpy(table).cuda(), torch.from_numpy(lut).cuda(), shift=3)
+    bucket = lut[np.clip(cols - rows - 3, -reach, reach) + reach]
+    g = rng.integers(-1, 2, (heads, rows.size)).astype(np.float16)
+    vals = torch.stack([fs.fs_csr_to_blk(fmt, torch.from_numpy(x).cuda()) for x in g])
+    want = np.stack([np.bincount(bucket, weights=x.astype(np.float64), minlength=n_buckets) for x in g]).astype(np.float16)
+    for _ in range(2):
+        assert np.array_equal(fs.fs_edge_bias_backward(fmt, vals, bias).cpu().numpy(), want)
+    got = fs.fs_edge_bias(fmt, vals, bias, scale=0.0)
+    for h in range(heads):
+        assert np.array_equal(fs.fs_blk_to_csr(fmt, got[h]).cpu().numpy(), table[h][bucket])
+
+
 def test_the_separate_calls_are_the_fused_one(fs):
     """SDDMM, bias, softmax, dropout, SpMM, and back: the same numbers up to the roundings in between."""
     import torch
