@@ -619,6 +619,11 @@ def fs_relative_buckets(buckets: int, max_distance: int, bidirectional: bool = T
     return torch.tensor(of[:0:-1] + [0] + behind, dtype=torch.uint8, device=device)
 
 
+def _beside(like, out, work):
+    """What the caller gave for an output and a workspace lies where the inputs do, the workspace in one piece."""
+    assert (out is None or out.device == like.device) and (work is None or (work.device == like.device and work.is_contiguous()))
+
+
 def _value_heads(fmt, vals):
     """Number of value arrays in (V*nvec,) or (heads, V*nvec)."""
     assert vals.is_cuda and vals.dtype == fmt.torch_dtype and vals.is_contiguous() and vals.dim() in (1, 2)
@@ -633,6 +638,7 @@ def fs_edge_bias(fmt: FsFormat, vals, bias: FsBucketBias, scale: float = 1.0, ou
         if got is not None:
             return _result(got, "fs_edge_bias")
     heads = _value_heads(fmt, vals)
+    _beside(vals, out, None)
     if out is None:
         out = torch.empty_like(vals)
     assert out.shape == vals.shape and out.dtype == vals.dtype and out.is_contiguous()
@@ -659,6 +665,7 @@ def fs_edge_bias_backward(fmt: FsFormat, grad, bias: FsBucketBias, out=None, wor
         if got is not None:
             return _result(got, "fs_edge_bias_backward")
     heads = _value_heads(fmt, grad)
+    _beside(grad, out, work)
     n_buckets = bias.table.shape[-1]
     if out is None:
         out = grad.new_empty((heads, n_buckets) if grad.dim() == 2 else (n_buckets,))
@@ -680,6 +687,7 @@ def fs_edge_dropout(fmt: FsFormat, vals, dropout: FsDropout, out=None, stream=No
         if got is not None:
             return _result(got, "fs_edge_dropout")
     heads = _value_heads(fmt, vals)
+    _beside(vals, out, None)
     if out is None:
         out = torch.empty_like(vals)
     assert out.shape == vals.shape and out.dtype == vals.dtype and out.is_contiguous()
@@ -718,7 +726,7 @@ def _attention_operands(fmt, X, Y, H, bias, dropout):
     x, heads, d = _head_matrix(X, fmt, fmt.c.M)
     y, kv_heads, dy = _head_matrix(Y, fmt, fmt.c.K)
     h, hv, N = _head_matrix(H, fmt, fmt.c.K)
-    assert dy == d and hv == kv_heads and X.dim() == Y.dim() == H.dim()
+    assert dy == d and hv == kv_heads and X.dim() == Y.dim() == H.dim() and X.device == Y.device == H.device
     return (heads, kv_heads, d, N, x, y, h, None if bias is None else ctypes.byref(bias._struct(fmt, heads)),
             None if dropout is None else ctypes.byref(dropout._struct()))
 
@@ -735,6 +743,8 @@ def fs_attention_forward(fmt: FsFormat, X, Y, H, scale: float = 1.0, bias: Optio
             return _result(got, "fs_attention_forward")
     heads, kv_heads, d, N, x, y, h, b, dr = _attention_operands(fmt, X, Y, H, bias, dropout)
     M = fmt.c.M
+    _beside(X, out, work)
+    _beside(X, lse, None)
     if out is None:
         out = X.new_empty((M, N) if X.dim() == 2 else (M, heads, N))
     assert out.dim() == X.dim()
@@ -770,6 +780,8 @@ def fs_attention_backward(fmt: FsFormat, fmt_t: FsFormat, X, Y, H, out, lse, gra
             return _result(got, "fs_attention_backward")
     heads, kv_heads, d, N, x, y, h, b, dr = _attention_operands(fmt, X, Y, H, bias, dropout)
     M = fmt.c.M
+    for t in (out, lse, grad, dX, dY, dH, dTable):
+        _beside(X, t, work)
     assert out.dim() == grad.dim() == X.dim()
     o, oh, oN = _head_matrix(out, fmt, M)
     g, gh, gN = _head_matrix(grad, fmt, M)

@@ -542,3 +542,27 @@ def test_refusals(fs):
                 lambda: fs.FsDropout(0.1, a.state.int()), lambda: fs.FsBucketBias(a.bias.table, a.bias.buckets[1:])):
         with pytest.raises(AssertionError):
             bad()
+
+
+def test_outputs_and_workspaces_elsewhere_are_refused(fs):
+    """Memory of the host, or a workspace with gaps, never becomes a kernel's argument."""
+    import torch
+    a = Problem(fs, 5, 40, 30, 2, 2, 16, 24, "f16", p=0.2, bias=(8, 5))
+    o, l = a.forward()
+    vals = torch.zeros(2, a.fmt.V * a.fmt.nvec, dtype=torch.float16, device="cuda")
+    gaps = torch.empty(1 << 20, dtype=torch.uint8, device="cuda")[::2]
+    host = torch.empty(1 << 20, dtype=torch.uint8)
+    run = dict(scale=a.scale, bias=a.bias, dropout=a.drop)
+    calls = [lambda: fs.fs_edge_bias(a.fmt, vals, a.bias, out=vals.cpu()), lambda: fs.fs_edge_dropout(a.fmt, vals, a.drop, out=vals.cpu()),
+             lambda: fs.fs_edge_bias_backward(a.fmt, vals, a.bias, out=a.bias.table.cpu()),
+             lambda: fs.fs_attention_forward(a.fmt, a.X, a.Y, a.H, out=o.cpu(), **run), lambda: fs.fs_attention_forward(a.fmt, a.X, a.Y, a.H, lse=l.cpu(), **run),
+             lambda: fs.fs_attention_forward(a.fmt, a.X, a.Y.cpu(), a.H, **run),
+             lambda: fs.fs_attention_backward(a.fmt, a.fmt_t, a.X, a.Y, a.H, o, l.cpu(), a.G, **run),
+             lambda: fs.fs_attention_backward(a.fmt, a.fmt_t, a.X, a.Y, a.H, o, l, a.G, dTable=a.bias.table.cpu(), **run)]
+    for work in (gaps, host):
+        calls += [lambda work=work: fs.fs_edge_bias_backward(a.fmt, vals, a.bias, work=work),
+                  lambda work=work: fs.fs_attention_forward(a.fmt, a.X, a.Y, a.H, work=work, **run),
+                  lambda work=work: fs.fs_attention_backward(a.fmt, a.fmt_t, a.X, a.Y, a.H, o, l, a.G, work=work, **run)]
+    for call in calls:
+        with pytest.raises(AssertionError):
+            call()
