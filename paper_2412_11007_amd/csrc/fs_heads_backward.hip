@@ -488,7 +488,7 @@ Pieces pieces_of(const fs_format *f, const fs_format *t, int64_t heads, int64_t 
     p.groups = (int)std::min<int64_t>(1024, (f->n_items + 31) / 32);
     p.sums = fs_align_up(2 * (size_t)heads * (size_t)f->M, 4);
     p.grouped = p.sums + fs_align_up((size_t)heads * (size_t)f->n_items * (size_t)n_grad, 4);
-    p.x = p.grouped + fs_align_up((size_t)heads * (size_t)p.groups * (size_t)n_grad, 4);
+    p.x = p.grouped + fs_align_up(fs_bucket_sums_floats(heads, p.groups, n_grad), 4);  // (with room for the sums' own launches)
     p.y = p.x + fs_part_floats(f, heads, d);
     p.h = p.y + fs_part_floats(t, kv_heads, d);
     p.total = p.h + fs_part_floats(t, kv_heads, N);

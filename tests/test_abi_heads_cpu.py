@@ -154,3 +154,17 @@ def test_workspace_sizes(fs):
     assert c.lib.fs_attention_backward_workspace_bytes(f, t, 4, 2, 16, 24, 8, ctypes.byref(n)) == 0
     assert n.value >= without + 4 * 4 * 13 * 8
     assert c.lib.fs_attention_backward_workspace_bytes(f, None, 4, 2, 16, 24, 0, ctypes.byref(n)) == 1
+
+
+@pytest.mark.parametrize("items", [1, 33, 5000, 16385, 40000])
+@pytest.mark.parametrize("buckets", [1, 32, 65, 128])
+def test_workspace_holds_every_launch_of_the_sums(fs, items, buckets):
+    """The wavefronts' sums, up to 1024 groups of them, and the 64 partial tables that two launches add those through."""
+    c = Call(fs)
+    n = ctypes.c_size_t(0)
+    c.fmt.n_items = items
+    f, t = ctypes.byref(c.fmt), ctypes.byref(c.fmt_t)
+    assert c.lib.fs_attention_backward_workspace_bytes(f, t, 4, 2, 16, 24, 0, ctypes.byref(n)) == 0
+    without = n.value
+    assert c.lib.fs_attention_backward_workspace_bytes(f, t, 4, 2, 16, 24, buckets, ctypes.byref(n)) == 0
+    assert n.value >= without + 4 * 4 * buckets * (items + min(1024, -(-items // 32)) + 64)

@@ -566,3 +566,28 @@ def test_outputs_and_workspaces_elsewhere_are_refused(fs):
     for call in calls:
         with pytest.raises(AssertionError):
             call()
+
+
+def test_sums_of_many_wavefronts_stay_in_the_workspace(fs):
+    """128 buckets and more than 16384 items: the sums go through two launches.  What lies behind the workspace is left alone."""
+    import torch
+    rng = np.random.default_rng(9)
+    M, deg = 120000, 6
+    cols = np.sort((np.arange(M)[:, None] * 7 + np.cumsum(rng.integers(1, 9000, (M, deg)), axis=1)) % M, axis=1)
+    at = np.unique(np.arange(M)[:, None] * M + cols)
+    rows, cols = at // M, at % M
+    rp = to_dev_i32(np.concatenate([[0], np.cumsum(np.bincount(rows, minlength=M))]))
+    ci = to_dev_i32(cols)
+    fmt = fs.fs_convert(rp, ci, None, M, M, torch_dtype=torch.float16, V=4, chunk=32)
+    rpt, cit, _ = fs.fs_csr_transpose(rp, ci, M, M)
+    fmt_t = fs.fs_convert(rpt, cit, None, M, M, torch_dtype=torch.float16, V=4)
+    assert fmt.n_items > 16384
+    X, Y, H, G = (torch.from_numpy(rng.standard_normal((M, 1, 8))).half().cuda() for _ in range(4))
+    lut = torch.from_numpy((np.arange(2049) % 128).astype(np.uint8)).cuda()
+    bias = fs.FsBucketBias(torch.from_numpy(rng.standard_normal((1, 128))).half().cuda(), lut)
+    o, l = fs.fs_attention_forward(fmt, X, Y, H, scale=0.3, bias=bias)
+    want = fs.fs_attention_backward(fmt, fmt_t, X, Y, H, o, l, G, scale=0.3, bias=bias)
+    need = fs.fs_attention_backward_workspace_bytes(fmt, fmt_t, 1, 1, 8, 8, 128)
+    store = torch.full((need + (1 << 20),), 0xA5, dtype=torch.uint8, device="cuda")
+    got = fs.fs_attention_backward(fmt, fmt_t, X, Y, H, o, l, G, scale=0.3, bias=bias, work=store[:need])
+    assert bool((store[need:] == 0xA5).all()) and all(torch.equal(a, b) for a, b in zip(got, want))
