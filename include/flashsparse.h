@@ -391,7 +391,8 @@ typedef struct fs_head_matrix {
  * positions outside the pattern get +0.0.  d_out_blk may be d_in_blk.  2-byte aligned arrays; scale is finite; heads >= 0.
  * fs_edge_bias_backward: the gradient of the table from the gradient g of out,
  *   grad[h * n_buckets + k] = sum of g over the entries of bucket k   (heads * n_buckets elements, rounded once; the bias's
- *   table is not read, its ld not looked at).  The gradient of `in` is scale * g.  d_work: fs_edge_bias_backward_workspace_bytes, 16-byte aligned.
+ *   table is not read, its ld not looked at).  The gradient of `in` is scale * g.  d_work:
+ *   fs_edge_bias_backward_workspace_bytes, 16-byte aligned.
  * Both are asynchronous on `stream` and deterministic (no atomics between wavefronts, sums in a fixed order).
  */
 fs_status fs_edge_bias(const fs_format *fmt, int32_t heads, const void *d_in_blk, float scale, const fs_bucket_bias *bias,
@@ -419,9 +420,10 @@ fs_status fs_edge_dropout(const fs_format *fmt, int32_t heads, const void *d_in_
  *   d_lse : heads x M floats, 4-byte aligned, or NULL; a row without entries gets zeros and minus infinity
  *   d_work : fs_attention_forward_workspace_bytes, 16-byte aligned (may be NULL when that size is 0)
  * out and d_lse overlap nothing that is read.  Scores and probabilities stay in registers in fp32; for the product with H a
- * probability is the sum of two numbers of the element type, the rounded one and what its rounding left.  M and K below 2^24; a head of X, Y and H spans less than 4 GiB, a row pitch is below
- * 2^24 bytes (else FS_ERR_UNSUPPORTED).  As in fs_spmm, an infinity or NaN in a row of H reaches all
- * rows of the windows that reference it; one in a row of X or Y reaches the scores of the entries it has, not their neighbours'.  Asynchronous on `stream`; deterministic.
+ * probability is the sum of two numbers of the element type, the rounded one and what its rounding left.  M and K below 2^24;
+ * a head of X, Y and H spans less than 4 GiB, a row pitch is below 2^24 bytes (else FS_ERR_UNSUPPORTED).  As in fs_spmm, an
+ * infinity or NaN in a row of H reaches all rows of the windows that reference it; one in a row of X or Y reaches the scores
+ * of the entries it has, not their neighbours'.  Asynchronous on `stream`; deterministic.
  */
 fs_status fs_attention_forward_workspace_bytes(const fs_format *fmt, int32_t heads, int64_t N, size_t *work_bytes);
 fs_status fs_attention_forward(const fs_format *fmt, int32_t heads, int32_t kv_heads, int64_t d, int64_t N, float scale,

@@ -16,7 +16,8 @@
 //
 // dtable: the block's dS pass through LDS, its stored elements are dealt out to the lanes, and each adds to one of 16 columns of a table of
 // fp32 sums, kSumColumns for each bucket.  Four lanes share a column and take turns, kept apart by fences (a column for each lane, 8 KB
-// with 32 buckets: gradients of a lognormal graph 1068 us for 1017; atomics on LDS: 51 us for 15 in the same sums over a value array).  A wavefront leaves one sum per bucket, and those are added in the order of the work list.
+// with 32 buckets: gradients of a lognormal graph 1068 us for 1017; atomics on LDS: 51 us for 15 in the same sums over a value array).  A wavefront
+// leaves one sum per bucket, and those are added in the order of the work list.
 //
 // By columns the query heads that share keys and values are walked inside a block, one after the other, into the same accumulators.
 //
