@@ -437,8 +437,9 @@ fs_status fs_attention_forward(const fs_format *fmt, int32_t heads, int32_t kv_h
  *   dX = scale * dS * Y,  dY = scale * dS^T * X,  dH = (Z * P)^T * G,  dtable[h][k] = sum of dS over bucket k,
  * dY and dH summed over the query heads that share them.  Two passes: by rows over fmt (dX, dtable) and by columns over
  * fmt_t, the format of A^T (fs_csr_transpose, fs_convert).  Scores are computed again from X and Y; dS and Z * P are rounded
- * to the element type for the products (fp16: loss scaling keeps dS out of its subnormal range).  An infinity or NaN in a row of Y,
- * X or G reaches the gradients of all rows of the windows that reference it.
+ * to the element type for the products (fp16: dS times a power of two of its row of the product, Z * P times 2^12, so that
+ * neither small gradients nor long rows lose them; an entry is off by at most 2^-36 of its row's largest beside its rounding).  An
+ * infinity or NaN in a row of Y, X or G reaches the gradients of all rows of the windows that reference it.
  *   X, Y, H, bias, drop, scale : as in the forward call, whose out and lse these are;  G : M x N for each of `heads`
  *   dX, dY, dH : written whole (zeros where nothing is stored), and overlap nothing that is read
  *   d_table_grad : heads * n_buckets elements in the element type, 2-byte aligned, or NULL

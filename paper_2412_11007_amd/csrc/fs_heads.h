@@ -420,6 +420,9 @@ struct fs_entries {
 __device__ __forceinline__ uint32_t fs_bit_mask(uint32_t m, int x) { return (uint32_t)__builtin_amdgcn_sbfe((int)m, x, 1); }
 __device__ __forceinline__ float fs_choose(uint32_t mask, float a, float b) { return __uint_as_float((mask & __float_as_uint(a)) | (~mask & __float_as_uint(b))); }
 
+// 1 / v for a power of two.
+__device__ __forceinline__ float fs_inverse_power(float v) { return __uint_as_float((254u << 23) - __float_as_uint(v)); }
+
 template <int NT>
 __device__ __forceinline__ void fs_clear(fs_f4 (&acc)[NT])
 {
@@ -442,6 +445,43 @@ __device__ __forceinline__ fs_frag fs_round8_rest(const float (&p)[8], const fs_
 #pragma unroll
     for (int x = 0; x < 8; x++) rest[x] = p[x] - fs_widen<DT>(rounded.e[x]);
     return fs_round8<DT>(rest);
+}
+
+// dS for the matrix cores.  fp16 holds it times a power of two `up` of the window row (the four lanes of a row have the same), and the row's
+// accumulators are sums of as much: an entry of a row of thousands, or of a small gradient, would be 0 or one of few subnormal numbers otherwise, a
+// large one an infinity, where their sums are numbers.  `up` brings the largest |dS| seen in the row to 2^11 .. 2^12 when it is set and lasts up to
+// 2^15; then the accumulators change with it, as a softmax's do with its maximum.  So what an entry loses below the normal numbers is at most
+// 2^-36 of the row's largest.  A row that has seen nothing but zeros has kUpUnset.  bf16 has fp32's exponents and is rounded as it is.
+constexpr float kUpUnset = 0x1p120f;
+template <int DT, int NT>
+__device__ __forceinline__ fs_frag fs_round8_up(const float (&ds)[8], float &up, fs_f4 (&acc)[NT])
+{
+    if constexpr (DT == FS_BF16) return fs_round8<DT>(ds);
+    float top = 0.f;
+#pragma unroll
+    for (int x = 0; x < 8; x++) top = fmaxf(top, fabsf(ds[x]));
+    if (__builtin_amdgcn_ballot_w64(top * up > 0x1p15f)) {  // rare: a row's first block, and a few in which it grows
+        top = fs_row_max(top);
+        const float to = top * up > 0x1p15f ? __uint_as_float((265u - (__float_as_uint(top) >> 23)) << 23) : up;  // 2^11 over top's power of two
+        const float by = to * fs_inverse_power(up);
+#pragma unroll
+        for (int t = 0; t < NT; t++) acc[t] = acc[t] * by;
+        up = to;
+    }
+    float v[8];
+#pragma unroll
+    for (int x = 0; x < 8; x++) v[x] = ds[x] * up;
+    return fs_round8<DT>(v);
+}
+// What takes `up` out of the accumulators.
+template <int DT>
+__device__ __forceinline__ float fs_down(float up) { return DT == FS_BF16 ? 1.f : fs_inverse_power(up); }
+template <int DT, int NT>
+__device__ __forceinline__ void fs_scale_down(fs_f4 (&acc)[NT], float up)
+{
+    if constexpr (DT == FS_BF16) return;
+#pragma unroll
+    for (int t = 0; t < NT; t++) acc[t] = acc[t] * fs_down<DT>(up);
 }
 
 // Accumulators -> rounded rows of an output of up to NC columns, by way of the tile's LDS.
