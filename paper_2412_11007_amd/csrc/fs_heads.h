@@ -148,12 +148,8 @@ __device__ __forceinline__ float fs_log_sum(float m, float l)
     return l == 0.f ? -INFINITY : 0.693147180559945309f * (m + __builtin_amdgcn_logf(l));
 }
 
-// A bias in units of log2, its lowest bit free for a flag (fs_entries).
-__device__ __forceinline__ float fs_flagless_log2(float b)
-{
-    const float t = b * 1.44269504088896340736f;
-    return t != t ? t : __uint_as_float(__float_as_uint(t) & ~1u);
-}
+// A bias in units of log2.
+__device__ __forceinline__ float fs_bias_log2(float b) { return b * 1.44269504088896340736f; }
 
 // Host side: the checked arguments as the kernels take them.
 inline fs_bias_args fs_bias_of(const fs_bucket_bias *b)
@@ -311,13 +307,15 @@ __device__ __forceinline__ uint32_t fs_row_bits(const fs_walk &a, int first_slot
 // the places are stored, and with eight rows a window half the lanes have none.  So every lane takes one entry at a time from a list in LDS
 // or one place at a time in row order, without a list: where more than half of the block is stored; with four rows, whose 128 places are
 // two turns; with eight rows and no dropout, where a place costs less than the list's chain (one row of 1028 entries, eight heads, 12.1 us with
-// the list, 10.5 without; R-MAT of 65 k rows 48 and 45; with dropout, R-MAT of 131 k rows, gradients 156 with and 171 without).  The results go to `value`, a
-// V x 32 tile of biases whose lowest bit says whether dropout keeps the entry (of the 24 bits of a mantissa, for a bias of 8 or 11).
+// the list, 10.5 without; R-MAT of 65 k rows 48 and 45; with dropout, R-MAT of 131 k rows, gradients 156 with and 171 without).  The results go to two
+// V x 32 tiles, the biases and whether dropout keeps the entry.  (The latter as the lowest bit of the bias would set apart what is kept and what is
+// dropped in the softmax itself: beside a bias far from zero that bit is worth more than the scores.)
 template <int V>
 struct fs_entries {
     static constexpr int kPitch = 36;  // floats from a row of `value` to the next: rows start in different banks
     uint16_t list[32 * V];             // vector | row << 5 | bucket << 9
     float value[V * kPitch] __attribute__((aligned(16)));
+    uint8_t kept[32 * V] __attribute__((aligned(8)));  // 1 or 0; without dropout not written
 
     // m: occupancy of row j.  Returns how many of the list's elements to take, the same in all lanes.
     __device__ __forceinline__ int make_list(uint32_t m, int lane_, bool draws)
@@ -344,12 +342,8 @@ struct fs_entries {
     {
         const int lane = fs_lane_here(lane_);
         auto bucket = [&](int j, int col) -> int { return fs_bucket_of(lut, b.reach, b.shift, T ? col : row0 + j, T ? row0 + j : col); };
-        auto keep = [&](int j, int col) -> uint32_t {
-            return fs_threefry<13>(key, (uint32_t)(T ? col : row0 + j), (uint32_t)(T ? row0 + j : col)).k0 >= drop.below ? 1u : 0u;
-        };
-        auto with = [](float bias, uint32_t kept) -> float {  // (infinities stay what they are)
-            const uint32_t v = __float_as_uint(bias);
-            return __uint_as_float((v & 0x7F800000u) == 0x7F800000u ? v : v | kept);
+        auto keep = [&](int j, int col) -> uint8_t {
+            return fs_threefry<13>(key, (uint32_t)(T ? col : row0 + j), (uint32_t)(T ? row0 + j : col)).k0 >= drop.below ? 1 : 0;
         };
         if (n == 32 * V) {
             const int c = lane & 31, j0 = lane >> 5;
@@ -372,7 +366,7 @@ struct fs_entries {
                 }
                 if (drop.state) {
 #pragma unroll
-                    for (int i = 0; i < P; i++) v[i] = with(v[i], keep(2 * (i0 + i) + j0, cols));
+                    for (int i = 0; i < P; i++) kept[64 * (i0 + i) + lane] = keep(2 * (i0 + i) + j0, cols);
                 }
 #pragma unroll
                 for (int i = 0; i < P; i++) value[(2 * (i0 + i) + j0) * kPitch + c] = v[i];
@@ -388,13 +382,19 @@ struct fs_entries {
                     v = table[k];
                     list[r] = (uint16_t)(code | k << 9);
                 }
-                if (drop.state) v = with(v, keep(j, col));
+                if (drop.state) kept[code] = keep(j, col);
                 value[j * kPitch + c] = v;
             }
         }
         FS_WAVE_SYNC();
     }
-    // of the lane's places: row j, vectors 8g .. 8g+7
+    // of the lane's places, row j, vectors 8g .. 8g+7: whether they are kept, in bit 0 of a byte each
+    __device__ __forceinline__ uint2 kept_bytes(int lane_) const
+    {
+        const int lane = fs_lane_here(lane_);
+        return *reinterpret_cast<const uint2 *>(kept + 32 * (lane & (V - 1)) + 8 * (lane >> 4));
+    }
+    // and their biases
     __device__ __forceinline__ void values(float (&v)[8], int lane_) const
     {
         const int lane = fs_lane_here(lane_);
@@ -415,6 +415,9 @@ struct fs_entries {
         to[1] = fs_f4{v[4], v[5], v[6], v[7]};
     }
 };
+
+// Place x of kept_bytes as 0 or ~0.
+__device__ __forceinline__ uint32_t fs_kept_mask(const uint2 &bytes, int x) { return (uint32_t)__builtin_amdgcn_sbfe((int)(x < 4 ? bytes.x : bytes.y), 8 * (x & 3), 1); }
 
 // Bit x of m as 0 or ~0, and a choice by it.
 __device__ __forceinline__ uint32_t fs_bit_mask(uint32_t m, int x) { return (uint32_t)__builtin_amdgcn_sbfe((int)m, x, 1); }

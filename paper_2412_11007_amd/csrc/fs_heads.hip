@@ -50,7 +50,7 @@ k_heads_forward(fs_walk a, fs_operand X, fs_operand Y, fs_operand H, int share, 
     // while the item is on its way: what does not depend on it
     if (bias.n_buckets > 0) {
         fs_load_buckets(bias, lut, lane, 64);
-        for (int i = lane; i < bias.n_buckets; i += 64) table[i] = fs_flagless_log2(fs_widen<DT>(bias.table[head * bias.ld + i]));
+        for (int i = lane; i < bias.n_buckets; i += 64) table[i] = fs_bias_log2(fs_widen<DT>(bias.table[head * bias.ld + i]));
     }
     const fs_key key = fs_drop_key(drop, head);
     const int nblk = it.y;
@@ -106,20 +106,15 @@ k_heads_forward(fs_walk a, fs_operand X, fs_operand Y, fs_operand H, int share, 
         FS_WAVE_SYNC();
         const uint32_t m8 = bits0 >> (8 * g);
         float p[8], mx = -INFINITY;
-        uint32_t kept[8];
+        uint2 kept = make_uint2(~0u, ~0u);
         if (looks_up) {
+            if (drop.state) kept = entries.kept_bytes(lane);
             entries.values(p, lane);
 #pragma unroll
-            for (int x = 0; x < 8; x++) {
-                kept[x] = drop.state ? fs_bit_mask(__float_as_uint(p[x]), 0) : ~0u;
-                p[x] = fmaf(sc[x >> 2][x & 3], sl2, p[x]);
-            }
+            for (int x = 0; x < 8; x++) p[x] = fmaf(sc[x >> 2][x & 3], sl2, p[x]);
         } else {
 #pragma unroll
-            for (int x = 0; x < 8; x++) {
-                kept[x] = ~0u;
-                p[x] = sc[x >> 2][x & 3] * sl2;
-            }
+            for (int x = 0; x < 8; x++) p[x] = sc[x >> 2][x & 3] * sl2;
         }
 #pragma unroll
         for (int x = 0; x < 8; x++) {
@@ -138,7 +133,7 @@ k_heads_forward(fs_walk a, fs_operand X, fs_operand Y, fs_operand H, int share, 
         l_run = l_run * corr + ps;
         m_run = m_new;
 #pragma unroll
-        for (int x = 0; x < 8; x++) p[x] = __uint_as_float(kept[x] & __float_as_uint(p[x]));
+        for (int x = 0; x < 8; x++) p[x] = __uint_as_float(fs_kept_mask(kept, x) & __float_as_uint(p[x]));
         const fs_frag hi = fs_round8<DT>(p), lo = fs_round8_rest<DT>(p, hi);
         if (d0.kb > 0) {
 #pragma unroll

@@ -62,7 +62,7 @@ k_heads_rows(fs_walk a, fs_operand X, fs_operand Y, fs_operand H, fs_operand out
     // while the item is on its way: what does not depend on it
     if (bias.n_buckets > 0) {
         fs_load_buckets(bias, lut, lane, 64);
-        for (int i = lane; i < bias.n_buckets; i += 64) table[i] = fs_flagless_log2(fs_widen<DT>(bias.table[head * bias.ld + i]));
+        for (int i = lane; i < bias.n_buckets; i += 64) table[i] = fs_bias_log2(fs_widen<DT>(bias.table[head * bias.ld + i]));
     }
     const fs_key key = fs_drop_key(drop, head);
     const int nblk = it.y;
@@ -159,16 +159,17 @@ k_heads_rows(fs_walk a, fs_operand X, fs_operand Y, fs_operand H, fs_operand out
         if (new_window) load_window(d1.w);
         const uint32_t m8 = bits0 >> (8 * g);
         float ds[8];
+        uint2 kept8 = make_uint2(~0u, ~0u);
         if (looks_up) {
+            if (drop.state) kept8 = entries.kept_bytes(lane);
             entries.values(ds, lane);
         } else {
 #pragma unroll
             for (int x = 0; x < 8; x++) ds[x] = 0.f;
         }
-        const uint32_t all = drop.state ? 0u : ~0u;
 #pragma unroll
         for (int x = 0; x < 8; x++) {
-            const uint32_t kept = all | fs_bit_mask(__float_as_uint(ds[x]), 0);
+            const uint32_t kept = fs_kept_mask(kept8, x);
             const float p = __builtin_amdgcn_exp2f(fmaf(sc[x >> 2][x & 3], sl2, ds[x]) - lse2);
             const float gz = __uint_as_float(kept & __float_as_uint(gp[x >> 2][x & 3]));
             ds[x] = __uint_as_float(fs_bit_mask(m8, x) & __float_as_uint(p * fmaf(gz, drop.factor, -D)));
@@ -250,7 +251,7 @@ k_heads_cols(fs_walk a, int64_t rows, fs_operand X, fs_operand Y, fs_operand H, 
     if (bias.n_buckets > 0) {
         fs_load_buckets(bias, lut, lane, 64);
         for (int i = lane; i < bias.n_buckets * share; i += 64)
-            table[i] = fs_flagless_log2(fs_widen<DT>(bias.table[(kv * share + i / bias.n_buckets) * bias.ld + i % bias.n_buckets]));
+            table[i] = fs_bias_log2(fs_widen<DT>(bias.table[(kv * share + i / bias.n_buckets) * bias.ld + i % bias.n_buckets]));
     }
     fs_key keys = fs_key{0u, 0u};  // lane i: that of the group's head i
     if (drop.state) {
@@ -327,16 +328,17 @@ k_heads_cols(fs_walk a, int64_t rows, fs_operand X, fs_operand Y, fs_operand H, 
         }
         const uint32_t m8 = bits0 >> (8 * g);
         float ds[8], w[8];
+        uint2 kept8 = make_uint2(~0u, ~0u);
         if (looks_up) {
+            if (drop.state) kept8 = entries.kept_bytes(lane);
             entries.values(ds, lane);
         } else {
 #pragma unroll
             for (int x = 0; x < 8; x++) ds[x] = 0.f;
         }
-        const uint32_t all = drop.state ? 0u : ~0u;
 #pragma unroll
         for (int x = 0; x < 8; x++) {
-            const uint32_t stored = fs_bit_mask(m8, x), kept = stored & (all | fs_bit_mask(__float_as_uint(ds[x]), 0));
+            const uint32_t stored = fs_bit_mask(m8, x), kept = stored & fs_kept_mask(kept8, x);
             const float2 rs = lds_stats[8 * g + x];
             const float p = __builtin_amdgcn_exp2f(fmaf(sc[x >> 2][x & 3], sl2, ds[x]) - rs.x);
             w[x] = __uint_as_float(kept & __float_as_uint(p * kWeight));
