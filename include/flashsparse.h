@@ -354,7 +354,9 @@ fs_status fs_attention(const fs_format *fmt,
  *               counts as that one
  *   n_buckets : 1 .. 128;  reach : 0 .. 1024
  *   shift     : |shift| < 2^31; the position of row 0 where the rows of A are the last ones of a sequence
- * A bias of minus infinity takes its entries out; a row of which nothing is left counts as one without entries.
+ * A bias of minus infinity takes its entries out; a row of which nothing is left counts as one without entries.  Finite
+ * biases, the type's lowest value among them, do not: a row that has nothing else has their probabilities.  In fs_attention_forward and
+ * its gradients 2.358e38 (the largest fp32 number over log2 e) counts for larger ones, lse included.
  */
 typedef struct fs_bucket_bias {
     const void *d_table;

@@ -148,8 +148,12 @@ __device__ __forceinline__ float fs_log_sum(float m, float l)
     return l == 0.f ? -INFINITY : 0.693147180559945309f * (m + __builtin_amdgcn_logf(l));
 }
 
-// A bias in units of log2.
-__device__ __forceinline__ float fs_bias_log2(float b) { return b * 1.44269504088896340736f; }
+// A bias in units of log2.  A finite one stays finite: bf16's lowest value is a mask, but no minus infinity.
+__device__ __forceinline__ float fs_bias_log2(float b)
+{
+    const float t = b * 1.44269504088896340736f;
+    return __builtin_isfinite(b) ? fminf(fmaxf(t, -3.402823466e38f), 3.402823466e38f) : t;
+}
 
 // Host side: the checked arguments as the kernels take them.
 inline fs_bias_args fs_bias_of(const fs_bucket_bias *b)

@@ -70,3 +70,13 @@ FAR = [("bf16", -1e30), ("bf16", -1e9), ("bf16", 1e9), ("bf16", -1e6), ("bf16", 
 def test_dropped_and_kept_entries_have_the_same_bias(fs, dtype, bias, V, V_t, chunk, share):  # noqa: F811
     """What dropout leaves of a row is weighted with the probabilities of all of it, also where the last bit of a bias is worth more than the scores."""
     check_forward(far_problem(fs, dtype, bias, V, V_t, chunk, share))
+
+
+LOWEST = 3.3895313892515355e38
+
+
+@pytest.mark.parametrize("bias", [-LOWEST, LOWEST, -2.5e38])
+@pytest.mark.parametrize("V,V_t,chunk,share", SHAPES)
+def test_the_lowest_finite_value_is_no_infinity(fs, bias, V, V_t, chunk, share):  # noqa: F811
+    """A row of nothing but the type's lowest value has the mean of its rows of H."""
+    check_forward(far_problem(fs, "bf16", bias, V, V_t, chunk, share))
