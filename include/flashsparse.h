@@ -440,7 +440,8 @@ fs_status fs_attention_forward(const fs_format *fmt, int32_t heads, int32_t kv_h
  * dY and dH summed over the query heads that share them.  Two passes: by rows over fmt (dX, dtable) and by columns over
  * fmt_t, the format of A^T (fs_csr_transpose, fs_convert).  Scores are computed again from X and Y; dS and Z * P are rounded
  * to the element type for the products (fp16: dS times a power of two of its row of the product, Z * P times 2^12, so that
- * neither small gradients nor long rows lose them; an entry is off by at most 2^-36 of its row's largest beside its rounding).  An
+ * neither small gradients nor long rows lose them; an entry is off by at most 2^-36 of its row's largest beside its rounding).
+ * Where |lse| is above 1000, a row's sum is worked out again: beside a mask of -1e9, say, lse holds nothing of it.  An
  * infinity or NaN in a row of Y, X or G reaches the gradients of all rows of the windows that reference it.
  *   X, Y, H, bias, drop, scale : as in the forward call, whose out and lse these are;  G : M x N for each of `heads`
  *   dX, dY, dH : written whole (zeros where nothing is stored), and overlap nothing that is read

@@ -38,17 +38,72 @@ namespace {
 constexpr int kSumColumns = 16;  // of the table of sums in LDS, for each bucket
 __host__ __device__ constexpr float fs_weight_scale(int dtype) { return dtype == FS_F16 ? 4096.f : 1.f; }  // of Z P
 
+// Rows far from zero.  Beside a maximum of a thousand an fp32 lse holds too little of the logarithm of a row's sum for exp(s - lse) to add up to
+// one, beside a mask of -1e9 nothing of it.  Of such rows, of |lse| > kFar, the maximum and the logarithm of the sum of 2^(s - maximum) are worked
+// out again and subtracted one after the other.  A wavefront of the walk by rows looks for them in its item's windows before it begins and
+// leaves both beside {lse, D}, for rows from kFarLeft on, with the maximum for lse.  The walk by columns finds them by what stands for their lse there, in units of log2 (kFarFound): of a
+// far row it is at most 24 from lse, log2 of the most entries of a row, so above 1418; of those not left there at most 1399.
+constexpr float kFar = 1000.f, kFarLeft = 970.f, kFarFound = 1410.f;
+__device__ __forceinline__ bool is_far(float lse, float limit) { return fabsf(lse) > limit && fabsf(lse) < INFINITY; }
+
+// Of the window's rows in lanes (j, g): the maximum of the scores, in units of log2, and the logarithm of the sum of 2^(s - maximum).  `at`: any block
+// slot of the window.  All blocks of the window are walked, whatever item they belong to, with the products of the walk itself (the same bits:
+// far from zero one more would be worth more than all), Y's rows straight from memory.  Rare: kept small, not fast.
+template <int DT, int V, int KS>
+__device__ __forceinline__ float2 far_rows(const fs_walk &a, int at, const unsigned char *Xb, uint32_t x_pitch, const unsigned char *Yb, uint32_t y_pitch, int d,
+                                           float sl2, const fs_bias_args &bias, const float *table, const uint8_t *lut, int lane)
+{
+    const int j = lane & 15, g = lane >> 4;
+    fs_frag xf[KS];
+    fs_load_window<V>(xf, Xb, x_pitch, d, a.blk_desc[at].z, a.M, lane);
+    while (!(a.blk_desc[at].y & 512)) at--;
+    float m = -INFINITY, l = 0.f;
+#pragma unroll 1
+    for (bool last = false; !last; at++) {
+        const int4 desc = a.blk_desc[at];
+        const int kb = desc.y & 255;
+        last = desc.y & 256;
+        const uint32_t m8 = j < V ? a.row_bits[(int64_t)at * V + (j & (V - 1))] >> (8 * g) : 0u;
+        auto column = [&](int v) -> int { return a.vec_col[max(min(desc.x + min(v, kb - 1), a.nvec - 1), 0)]; };
+#pragma unroll
+        for (int t = 0; t < 2; t++) {
+            const unsigned char *row = Yb + fs_mul24((uint32_t)column(8 * (j >> 2) + (j & 3) + 4 * t), y_pitch);
+            fs_f4 sc = fs_f4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int ks = 0; ks < KS; ks++) {
+                fs_frag y;
+                y.u = fs_u4{0u, 0u, 0u, 0u};
+                if (32 * ks + 8 * g < d) y.u = *reinterpret_cast<const fs_u4 *>(row + 64 * ks + 16 * g);
+                sc = fs_mfma_16x16x32<DT>(y, xf[ks], sc);
+            }
+#pragma unroll
+            for (int k = 0; k < 4; k++) {
+                if (!(m8 >> (4 * t + k) & 1u)) continue;
+                const int col = column(8 * g + 4 * t + k);
+                const float s = fmaf(sc[k], sl2, bias.n_buckets > 0 ? table[fs_bucket_of(lut, bias.reach, bias.shift, desc.z * V + j, col)] : 0.f);
+                const float m_new = fmaxf(m, s), use = m_new == -INFINITY ? 0.f : m_new;
+                l = l * __builtin_amdgcn_exp2f(m - use) + __builtin_amdgcn_exp2f(s - use);
+                m = m_new;
+            }
+        }
+    }
+    const float top = fs_row_max(m);
+    l = fs_row_sum(l * __builtin_amdgcn_exp2f(m - (top == -INFINITY ? 0.f : top)));
+    return make_float2(top, __builtin_amdgcn_logf(l));
+}
+
 template <int DT, int V, int KS, int NT>
 __global__ void __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(KS <= 2 && NT <= 4 ? 4 : KS * NT <= 8 ? 3 : 2)))
 k_heads_rows(fs_walk a, fs_operand X, fs_operand Y, fs_operand H, fs_operand out, fs_operand G, const float *__restrict__ lse, int share, int d, int N,
-             float sl2, float scale, fs_bias_args bias, fs_drop_args drop, fs_operand dX, float2 *__restrict__ row_stats, float *__restrict__ part,
-             float *__restrict__ bucket_sums)
+             float sl2, float scale, fs_bias_args bias, fs_drop_args drop, fs_operand dX, float2 *__restrict__ row_stats, float2 *far,
+             float *__restrict__ part, float *__restrict__ bucket_sums)
 {
     using tile_y = fs_gathered<32 * KS>;
     using tile_h = fs_gathered<16 * NT>;
     constexpr int KN = NT / 2, COLS = kSumColumns;
     __shared__ __attribute__((aligned(16))) unsigned char lds[tile_y::kBytes > tile_h::kBytes ? tile_y::kBytes : tile_h::kBytes];  // H's rows, then Y's
     __shared__ __attribute__((aligned(16))) int lds_cols[32];
+    __shared__ float2 lds_far[16];  // by window row
     __shared__ fs_entries<V> entries;
     extern __shared__ __attribute__((aligned(16))) unsigned char dyn[];
     float *table = reinterpret_cast<float *>(dyn);
@@ -103,10 +158,30 @@ k_heads_rows(fs_walk a, fs_operand X, fs_operand Y, fs_operand H, fs_operand out
     };
     load_window(d0.w);
     load_stats(d0.w);
+    // whether the item's windows have a far row
+    bool item_far = false;
+    {
+        const float *of = lse + (int64_t)head * a.M;
+        const int last = min((__builtin_amdgcn_readlane(my_desc.z, nblk - 1) + 1) * V, (int)a.M) - 1;
+        for (int first = d0.w * V; first <= last; first += 64) item_far |= is_far(of[min(first + lane, last)], kFarLeft);
+    }
     tile_y y;
     tile_h h;
     y.load(Yb, Y.pitch, y_colb, cols0, lane);
     h.load(Hb, H.pitch, h_colb, cols0, lane);
+    item_far = __builtin_amdgcn_ballot_w64(item_far);
+    if (__builtin_expect(item_far, 0)) {
+        FS_WAVE_SYNC();
+        for (int i = 0; i < nblk; i++) {  // (a window's wavefronts all leave the same)
+            if (i > 0 && !block(i).first) continue;
+            const int64_t row = (int64_t)block(i).w * V + j;
+            const float2 got = far_rows<DT, V, KS>(a, it.x + i, Xb, X.pitch, Yb, Y.pitch, d, sl2, bias, table, lut, lane);
+            const float of_row = j < V && row < a.M ? lse[(int64_t)head * a.M + row] : 0.f;
+            if (g == 0 && is_far(of_row, kFarLeft))
+                far[(int64_t)head * a.M + row] = is_far(of_row, kFar) ? got : make_float2(of_row * 1.44269504088896340736f, 0.f);
+        }
+        __threadfence();
+    }
     const bool looks_up = bias.n_buckets > 0 || drop.state;
 
     fs_f4 acc[2 * KS];
@@ -153,7 +228,15 @@ k_heads_rows(fs_walk a, fs_operand X, fs_operand Y, fs_operand H, fs_operand out
             D = fs_row_sum(D);
             // a row of which nothing is left: exp(s - lse) has to come out as zero
             lse2 = my_lse == -INFINITY ? INFINITY : my_lse * 1.44269504088896340736f;
+            if (__builtin_expect(item_far, 0)) {
+                const bool left = j < V && row < a.M && is_far(my_lse, kFarLeft);
+                const float2 of_row = left ? far[(int64_t)head * a.M + row] : make_float2(lse2, 0.f);
+                lse2 = of_row.x;
+                if (const int l = fs_lane_here(lane); l < 16) lds_far[l] = of_row;
+                FS_WAVE_SYNC();
+            }
             if (d0.first && g == 0 && j < V && row < a.M) row_stats[(int64_t)head * a.M + row] = make_float2(lse2, D);
+            if (__builtin_expect(item_far, 0)) lse2 = 0.f;  // (see below)
         }
         new_window = MORE && d1.w != d0.w;
         if (new_window) load_window(d1.w);
@@ -166,6 +249,14 @@ k_heads_rows(fs_walk a, fs_operand X, fs_operand Y, fs_operand H, fs_operand out
         } else {
 #pragma unroll
             for (int x = 0; x < 8; x++) ds[x] = 0.f;
+        }
+        if (__builtin_expect(item_far, 0)) {  // the entries' exponents in place of their biases, beside a score and an lse of zero
+            const float2 of_row = lds_far[fs_lane_here(lane) & 15];
+#pragma unroll
+            for (int x = 0; x < 8; x++) {
+                ds[x] = (fmaf(sc[x >> 2][x & 3], sl2, ds[x]) - of_row.x) - of_row.y;
+                sc[x >> 2][x & 3] = 0.f;
+            }
         }
 #pragma unroll
         for (int x = 0; x < 8; x++) {
@@ -227,8 +318,8 @@ k_heads_rows(fs_walk a, fs_operand X, fs_operand Y, fs_operand H, fs_operand out
 // By columns: `a` walks A^T, its vectors are rows of A (`rows` of them) and its window rows columns.
 template <int DT, int V, int KS, int NT>
 __global__ void __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(KS <= 2 && NT <= 4 ? 3 : 2)))
-k_heads_cols(fs_walk a, int64_t rows, fs_operand X, fs_operand Y, fs_operand H, fs_operand G, const float2 *__restrict__ row_stats, int share, int d,
-             int N, float sl2, float scale, fs_bias_args bias, fs_drop_args drop, fs_operand dY, fs_operand dH, float *__restrict__ part_y,
+k_heads_cols(fs_walk a, int64_t rows, fs_operand X, fs_operand Y, fs_operand H, fs_operand G, const float2 *__restrict__ row_stats, const float2 *__restrict__ far,
+             int share, int d, int N, float sl2, float scale, fs_bias_args bias, fs_drop_args drop, fs_operand dY, fs_operand dH, float *__restrict__ part_y,
              float *__restrict__ part_h)
 {
     using tile_x = fs_gathered<32 * KS>;
@@ -301,6 +392,7 @@ k_heads_cols(fs_walk a, int64_t rows, fs_operand X, fs_operand Y, fs_operand H, 
             lds_rows[l] = rows0;
             lds_stats[l] = st;
         }
+        const float lse_here = st.x;  // of vector l mod 32
         BlockDesc d2 = d1;
         int rows2 = rows1;
         uint32_t bits2 = bits1;
@@ -335,6 +427,23 @@ k_heads_cols(fs_walk a, int64_t rows, fs_operand X, fs_operand Y, fs_operand H, 
         } else {
 #pragma unroll
             for (int x = 0; x < 8; x++) ds[x] = 0.f;
+        }
+        if (__builtin_expect(__builtin_amdgcn_ballot_w64(is_far(lse_here, kFarFound)) != 0, 0)) {
+            // the exponents of far rows' entries in place of their biases, beside a score and an lse of zero; the logarithms by way of lds_rows, which
+            // this head's entries are done with
+            const int l = fs_lane_here(lane);
+            if (l < 32) lds_rows[l] = is_far(lse_here, kFarFound) ? __float_as_int(far[(int64_t)(kv * share + member) * rows + rows0].y) : 0;
+            FS_WAVE_SYNC();
+#pragma unroll
+            for (int x = 0; x < 8; x++) {
+                const float of_row = lds_stats[8 * g + x].x;
+                if (!is_far(of_row, kFarFound)) continue;
+                ds[x] = (fmaf(sc[x >> 2][x & 3], sl2, ds[x]) - of_row) - __int_as_float(lds_rows[8 * g + x]);
+                sc[x >> 2][x & 3] = 0.f;
+            }
+            FS_WAVE_SYNC();
+            if (l < 32 && is_far(lse_here, kFarFound)) lds_stats[l].x = 0.f;
+            FS_WAVE_SYNC();
         }
 #pragma unroll
         for (int x = 0; x < 8; x++) {
@@ -486,17 +595,18 @@ __global__ void __launch_bounds__(64) k_heads_finish(Parts x, Parts y, Parts h, 
     add_sums(s, group - h.groups, head);
 }
 
-// Where the workspace's pieces lie, in floats: {lse, D} per row and head, the wavefronts' sums per bucket and the groups they are gathered
-// into, the partial tiles of the three outputs.
+// Where the workspace's pieces lie, in floats: {lse, D} per row and head, what far rows leave beside, the wavefronts' sums per bucket and the groups
+// they are gathered into, the partial tiles of the three outputs.
 struct Pieces {
-    size_t sums, grouped, x, y, h, total;
+    size_t far, sums, grouped, x, y, h, total;
     int groups;
 };
 Pieces pieces_of(const fs_format *f, const fs_format *t, int64_t heads, int64_t kv_heads, int64_t d, int64_t N, int64_t n_grad)
 {
     Pieces p;
     p.groups = (int)std::min<int64_t>(1024, (f->n_items + 31) / 32);
-    p.sums = fs_align_up(2 * (size_t)heads * (size_t)f->M, 4);
+    p.far = 2 * (size_t)heads * (size_t)f->M;
+    p.sums = fs_align_up(2 * p.far, 4);
     p.grouped = p.sums + fs_align_up((size_t)heads * (size_t)f->n_items * (size_t)n_grad, 4);
     p.x = p.grouped + fs_align_up(fs_bucket_sums_floats(heads, p.groups, n_grad), 4);  // (with room for the sums' own launches)
     p.y = p.x + fs_part_floats(f, heads, d);
@@ -518,7 +628,8 @@ fs_status rows_launch(const fs_format *f, const call &c, const Pieces &at)
     const size_t lds = (fs_bias_lds_bytes(c.bias.n_buckets, c.bias.reach) + 15) / 16 * 16 + (size_t)c.n_grad * 4 * kSumColumns;
     k_heads_rows<DT, V, KS, NT><<<dim3(geo.nbx, c.heads), 64, lds, c.st>>>(fs_walk_of(f, geo), c.X, c.Y, c.H, c.out, c.G, c.lse, c.heads / c.kv_heads, c.d, c.N,
                                                                           c.scale * 1.44269504088896340736f, c.scale, c.bias, c.drop, c.dX, (float2 *)c.work,
-                                                                          c.work + at.x, c.n_grad > 0 ? c.work + at.sums : nullptr);
+                                                                          (float2 *)(c.work + at.far), c.work + at.x,
+                                                                          c.n_grad > 0 ? c.work + at.sums : nullptr);
     FS_LAUNCH_CHECK();
     return FS_OK;
 }
@@ -529,9 +640,10 @@ fs_status cols_launch(const fs_format *f, const fs_format *t, const call &c, con
     const fs_launch_geometry geo = fs_launch_geometry_for(t, 1);
     const int share = c.heads / c.kv_heads;
     const size_t lds = c.bias.n_buckets > 0 ? fs_bias_lds_bytes(c.bias.n_buckets, c.bias.reach) + 4 * (size_t)c.bias.n_buckets * (share - 1) : 0;
-    k_heads_cols<DT, V, KS, NT><<<dim3(geo.nbx, c.kv_heads), 64, lds, c.st>>>(fs_walk_of(t, geo), f->M, c.X, c.Y, c.H, c.G, (const float2 *)c.work, share, c.d, c.N,
-                                                                             c.scale * 1.44269504088896340736f, c.scale, c.bias, c.drop, c.dY, c.dH, c.work + at.y,
-                                                                             c.work + at.h);
+    k_heads_cols<DT, V, KS, NT><<<dim3(geo.nbx, c.kv_heads), 64, lds, c.st>>>(fs_walk_of(t, geo), f->M, c.X, c.Y, c.H, c.G, (const float2 *)c.work,
+                                                                             (const float2 *)(c.work + at.far), share, c.d, c.N,
+                                                                             c.scale * 1.44269504088896340736f, c.scale, c.bias, c.drop, c.dY, c.dH,
+                                                                             c.work + at.y, c.work + at.h);
     FS_LAUNCH_CHECK();
     return FS_OK;
 }

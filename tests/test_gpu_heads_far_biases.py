@@ -80,3 +80,43 @@ LOWEST = 3.3895313892515355e38
 def test_the_lowest_finite_value_is_no_infinity(fs, bias, V, V_t, chunk, share):  # noqa: F811
     """A row of nothing but the type's lowest value has the mean of its rows of H."""
     check_forward(far_problem(fs, "bf16", bias, V, V_t, chunk, share))
+
+
+@pytest.mark.parametrize("dtype,bias", FAR + [("bf16", -LOWEST), ("bf16", LOWEST)])
+@pytest.mark.parametrize("V,V_t,chunk,share", SHAPES)
+def test_gradients_of_rows_whose_biases_are_all_far_from_zero(fs, dtype, bias, V, V_t, chunk, share):  # noqa: F811
+    """Such a row's lse holds nothing of what its probabilities add up to."""
+    check_gradients(far_problem(fs, dtype, bias, V, V_t, chunk, share))
+
+
+def test_probabilities_beside_a_far_bias_add_up_to_one(fs):  # noqa: F811
+    """A head with a bias of -30000 everywhere: a score keeps eight binary places beside it, a row's probabilities are those of such scores.  With a
+    gradient of out that is one in column i of row i alone, column i of dH holds row i's probabilities: each is rounded twice, and what
+    they are made of is off by 2^-15 in fp32."""
+    import torch
+    a = Problem(fs, 37, 32, 120, 2, 2, 32, 32, "f16", kind="dense", bias=(3, 10), chunk=64)
+    a.bias.table[1] = -30000.0
+    a.G.zero_()
+    a.G[torch.arange(32), :, torch.arange(32)] = 1.0
+    out, lse = a.forward()
+    total = a.f64(a.backward(out, lse)[2]).sum(0)
+    assert np.abs(total - 1).max() <= 2 * 2.0 ** -11 + 2.0 ** -15 + 120 * 2.0 ** -25
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("V,V_t,chunk,share", SHAPES)
+def test_rows_whose_scores_are_far_from_zero_without_a_bias(fs, dtype, V, V_t, chunk, share):  # noqa: F811
+    """Scores of some thousands that differ by a few: whole numbers below 2^24 times a power of two, so that X Y^T is exact and a score, in units of
+    log2, is off by 2^-24 of itself; so is a row's largest."""
+    rng = np.random.default_rng(6)
+    a = Problem(fs, 39, 90, 200, 2, 2 // share, 32, 48, dtype, kind="hub", p=0.25, V=V, V_t=V_t, chunk=chunk)
+    a.scale = a.ref.scale = 2.0 ** -4
+    X, Y = 32 * np.sign(rng.standard_normal((90, 2, 1))) * np.ones((90, 2, 32)), 64 + np.zeros((200, 2 // share, 32))
+    Y[:, :, :2] += rng.integers(-1, 2, (200, 2 // share, 2)) * 0.5
+    with_operands(a, X=X, Y=Y)
+    s = a.ref.scores(0)[0]
+    far = np.abs(s[a.stored])
+    assert far.min() > 4000 and far.max() < 4200
+    real = a.ref.scores
+    a.ref.scores = lambda h: (real(h)[0], np.zeros_like(s))
+    check_gradients(a, l_off=2.0 ** -22 * 4200)
