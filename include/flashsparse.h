@@ -422,7 +422,8 @@ fs_status fs_edge_dropout(const fs_format *fmt, int32_t heads, const void *d_in_
  *   d_lse : heads x M floats, 4-byte aligned, or NULL; a row without entries gets zeros and minus infinity
  *   d_work : fs_attention_forward_workspace_bytes, 16-byte aligned (may be NULL when that size is 0)
  * out and d_lse overlap nothing that is read.  Scores and probabilities stay in registers in fp32; for the product with H a
- * probability is the sum of two numbers of the element type, the rounded one and what its rounding left.  M and K below 2^24;
+ * probability is the sum of two numbers of the element type, the rounded one and what its rounding left (fp16: of 2^12 times a
+ * probability relative to its row's largest, of which 2^-25 is the least that either holds).  M and K below 2^24;
  * a head of X, Y and H spans less than 4 GiB, a row pitch is below 2^24 bytes (else FS_ERR_UNSUPPORTED).  As in fs_spmm, an
  * infinity or NaN in a row of H reaches all rows of the windows that reference it; one in a row of X or Y reaches the scores
  * of the entries it has, not their neighbours'.  Asynchronous on `stream`; deterministic.

@@ -7,7 +7,7 @@
 //   * the 32 rows of Y and of H are gathered row by row and put to LDS while the ones before are computed with;
 //   * the scores of the V x 32 block come from the matrix cores, Y's rows as the left operand and the window's rows of X, held in
 //     registers, as the right one: lane (j, g) gets the scores of window row j and vectors 8g .. 8g+7;
-//   * bias and pattern are applied in fp32 in units of log2, the running maximum m and sum l of the row are updated, the
+//   * bias and pattern are applied in fp32 in units of log2, the running maximum m (fp16: less 12) and sum l of the row are updated, the
 //     probabilities that dropout keeps become two numbers of the element type, the rounded one and what the rounding left;
 //   * both meet H's rows, read transposed from LDS, on the matrix cores; the accumulators are scaled by 2^(m_old - m_new).
 //     (The second product costs 3 to 7 %.  Without it the rounding of P would be in out beside out's own, and through D = g . out, whose
@@ -28,6 +28,11 @@
 #include "fs_heads.h"
 
 namespace {
+
+// What a row's probabilities are held relative to, given its largest score so far: fp16 holds them times 2^12, since beside a sink those of
+// thousands of entries would lie below its smallest number.  (Far from zero, where 12 less would be rounded, they are as they are.)
+template <int DT>
+__device__ __forceinline__ float reference_of(float top) { return DT == FS_F16 && fabsf(top) < 0x1p20f ? top - 12.f : top; }
 
 template <int DT, int V, int KS, int NT>
 __global__ void __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(KS <= 2 && NT <= 4 ? 4 : KS * NT <= 16 ? 3 : 2)))
@@ -78,7 +83,7 @@ k_heads_forward(fs_walk a, fs_operand X, fs_operand Y, fs_operand H, int share, 
 
     fs_f4 acc[NT];
     fs_clear(acc);
-    float m_run = -INFINITY, l_run = 0.f;  // l_run: this lane's share
+    float m_run = -INFINITY, l_run = 0.f;  // the largest reference so far; this lane's share of the sum relative to it
     bool from_first = d0.first;
     int step = 0;
     auto block_step = [&](auto more_) {
@@ -121,7 +126,7 @@ k_heads_forward(fs_walk a, fs_operand X, fs_operand Y, fs_operand H, int share, 
             p[x] = fs_choose(fs_bit_mask(m8, x), p[x], -INFINITY);
             mx = fmaxf(mx, p[x]);
         }
-        const float m_new = fmaxf(m_run, fs_row_max(mx));
+        const float m_new = fmaxf(m_run, reference_of<DT>(fs_row_max(mx)));
         const float m_use = m_new == -INFINITY ? 0.f : m_new;  // nothing seen so far
         const float corr = __builtin_amdgcn_exp2f(m_run - m_use);
         float ps = 0.f;

@@ -41,8 +41,9 @@ __host__ __device__ constexpr float fs_weight_scale(int dtype) { return dtype ==
 // Rows far from zero.  Beside a maximum of a thousand an fp32 lse holds too little of the logarithm of a row's sum for exp(s - lse) to add up to
 // one, beside a mask of -1e9 nothing of it.  Of such rows, of |lse| > kFar, the maximum and the logarithm of the sum of 2^(s - maximum) are worked
 // out again and subtracted one after the other.  A wavefront of the walk by rows looks for them in its item's windows before it begins and
-// leaves both beside {lse, D}, for rows from kFarLeft on, with the maximum for lse.  The walk by columns finds them by what stands for their lse there, in units of log2 (kFarFound): of a
-// far row it is at most 24 from lse, log2 of the most entries of a row, so above 1418; of those not left there at most 1399.
+// leaves both beside {lse, D}, for rows from kFarLeft on, with the maximum for lse.  The walk by columns finds them by what stands for their lse
+// there, in units of log2 (kFarFound): of a far row it is at most 24 from lse, log2 of the most entries of a row, so above 1418; of those not left there
+// at most 1399.
 constexpr float kFar = 1000.f, kFarLeft = 970.f, kFarFound = 1410.f;
 __device__ __forceinline__ bool is_far(float lse, float limit) { return fabsf(lse) > limit && fabsf(lse) < INFINITY; }
 
