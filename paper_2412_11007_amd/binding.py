@@ -701,7 +701,7 @@ def _head_matrix(t, fmt, rows):
     """(rows, columns) or (rows, heads, columns) -> (struct, heads, columns)."""
     assert t.is_cuda and t.dtype == fmt.torch_dtype and t.dim() in (2, 3) and t.shape[0] == rows and (t.stride(-1) == 1 or rows == 0)
     heads, columns = (t.shape[1], t.shape[2]) if t.dim() == 3 else (1, t.shape[1])
-    ld = heads * columns if rows == 0 else t.stride(0) if rows > 1 else max(t.stride(0), columns)  # (nothing is read by a stride that nothing needs)
+    ld = heads * columns if rows == 0 else t.stride(0) if rows > 1 else columns  # (nothing is read by a stride that nothing needs)
     head = 0 if t.dim() == 2 else columns if rows == 0 or heads == 1 else t.stride(1)
     return _FsHeadMatrix(t.data_ptr(), ld, head), heads, columns
 

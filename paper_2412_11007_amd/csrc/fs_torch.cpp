@@ -9,7 +9,6 @@
 // the binding's checks in Python then name.
 #include <Python.h>
 
-#include <algorithm>
 #include <initializer_list>
 
 #include <ATen/core/Tensor.h>
@@ -230,7 +229,7 @@ struct Heads {
         heads = dim == 3 ? t.size(1) : 1;
         columns = t.size(dim - 1);
         m.d = t.data_ptr();
-        m.ld = rows == 0 ? heads * columns : rows > 1 ? t.stride(0) : std::max(t.stride(0), columns);  // (nothing is read by a stride that nothing needs)
+        m.ld = rows == 0 ? heads * columns : rows > 1 ? t.stride(0) : columns;  // (nothing is read by a stride that nothing needs)
         m.head = dim == 2 ? 0 : rows == 0 || heads == 1 ? columns : t.stride(1);
         ok = true;
     }
