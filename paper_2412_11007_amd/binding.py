@@ -200,11 +200,22 @@ _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)  # a torch wi
 _current_device = getattr(torch._C, "_cuda_getDevice", None)        # package imports, and the first call raises
 
 
-def _stream_ptr(stream) -> int:
-    """Handle of ``stream``, or of the current device's current stream."""
+def _stream_ptr(stream, fmt=None) -> int:
+    """Handle of ``stream``, or of the current device's current stream; of the device that ``fmt`` lies on, where it is given."""
     if stream is not None:
+        assert fmt is None or getattr(stream, "device", fmt.arena.device) == fmt.arena.device
         return int(stream.cuda_stream)
-    return _raw_stream(_current_device()) if _raw_stream else torch.cuda.current_stream().cuda_stream
+    if not _raw_stream:
+        return torch.cuda.current_stream().cuda_stream
+    device = _current_device()
+    assert fmt is None or fmt.arena.device.index == device, "the format lies on another device than the current one"
+    return _raw_stream(device)
+
+
+def _here(fmt, *tensors):
+    """What a call is given lies on one device, the format's: a pointer does not tell, and a kernel would read another GPU's memory or the host's."""
+    home = fmt.arena.device
+    assert all(t is None or t.device == home for t in tensors)
 
 
 def _temporary(nbytes, like, stream):
@@ -312,6 +323,7 @@ def fs_convert(rowptr, colidx, vals, M: int, K: int, torch_dtype=None, V: int = 
     assert rowptr.dtype == torch.int32 and colidx.dtype == torch.int32 and rowptr.is_cuda and colidx.is_cuda
     assert rowptr.is_contiguous() and colidx.is_contiguous() and rowptr.numel() == M + 1
     assert vals is None or (vals.is_cuda and vals.is_contiguous() and vals.numel() == nnz)
+    assert all(t is None or t.device == rowptr.device for t in (colidx, vals, arena, scratch))
     a_bytes, s_bytes = fs_format_bytes(M, nnz, V, KB, code)
     dev = rowptr.device
     if arena is None:
@@ -342,9 +354,10 @@ def fs_spmm(fmt: FsFormat, B, vals=None, out=None, work=None, stream=None, event
     which records them around the main kernel.
     """
     if out is None and work is None and events is None:
-        got = _calls().spmm(ctypes.addressof(fmt.c), B, vals, stream, _stream_ptr(stream))
+        got = _calls().spmm(ctypes.addressof(fmt.c), fmt.arena, B, vals, stream, _stream_ptr(stream))
         if got is not None:
             return _result(got, "fs_spmm")
+    _here(fmt, B, vals, out, work)
     K, N = B.shape
     assert B.is_cuda and B.dtype == fmt.torch_dtype and B.stride(1) == 1 and K == fmt.c.K
     if out is None:
@@ -369,6 +382,7 @@ def bind_spmm(fmt: FsFormat, B, out, work=None, vals=None, stream=None):
     """fs_spmm with its arguments checked and marshalled once: returns a callable that only makes the C call
     (for loops that repeat one call and cannot afford the per-call checks of ``fs_spmm``).  The tensors must
     stay alive and unchanged in place; the stream is the one current now unless given."""
+    _here(fmt, B, vals, out, work)
     K, N = B.shape
     assert B.is_cuda and B.dtype == fmt.torch_dtype and B.stride(1) == 1 and K == fmt.c.K
     assert out.shape == (fmt.c.M, N) and out.stride(1) == 1 and out.dtype == B.dtype
@@ -388,6 +402,7 @@ def bind_spmm(fmt: FsFormat, B, out, work=None, vals=None, stream=None):
 
 def bind_sddmm(fmt: FsFormat, X, Y, out=None, out_csr=None, stream=None):
     """fs_sddmm marshalled once (see bind_spmm); at least one of ``out`` (blocked layout) and ``out_csr``."""
+    _here(fmt, X, Y, out, out_csr)
     assert X.is_cuda and Y.is_cuda and X.dtype == fmt.torch_dtype and Y.dtype == fmt.torch_dtype
     assert X.shape[0] == fmt.c.M and Y.shape[0] == fmt.c.K and X.shape[1] == Y.shape[1]
     assert X.stride(1) == 1 and Y.stride(1) == 1 and (out is not None or out_csr is not None)
@@ -408,6 +423,7 @@ def bind_sddmm(fmt: FsFormat, X, Y, out=None, out_csr=None, stream=None):
 
 def fs_spmm_static(fmt: FsFormat, B, out, vals=None, stream=None):
     """C = A @ B into ``out`` with the library's own fixed workspace: the call itself allocates nothing."""
+    _here(fmt, B, vals, out)
     K, N = B.shape
     assert B.is_cuda and B.dtype == fmt.torch_dtype and B.stride(1) == 1 and K == fmt.c.K
     assert out.shape == (fmt.c.M, N) and out.stride(1) == 1 and out.dtype == B.dtype
@@ -423,9 +439,10 @@ def fs_sddmm(fmt: FsFormat, X, Y, out=None, stream=None, out_csr=None, blocked=T
     ``out_csr`` (nnz elements) additionally receives them in CSR order from the same kernel.  With
     ``blocked=False`` only ``out_csr`` is written (allocated if not given) and returned."""
     if out is None and out_csr is None:
-        got = _calls().sddmm(ctypes.addressof(fmt.c), X, Y, bool(blocked), _stream_ptr(stream))
+        got = _calls().sddmm(ctypes.addressof(fmt.c), fmt.arena, X, Y, bool(blocked), _stream_ptr(stream))
         if got is not None:
             return _result(got, "fs_sddmm")
+    _here(fmt, X, Y, out, out_csr)
     assert X.is_cuda and Y.is_cuda and X.dtype == fmt.torch_dtype and Y.dtype == fmt.torch_dtype
     assert X.shape[0] == fmt.c.M and Y.shape[0] == fmt.c.K and X.shape[1] == Y.shape[1]
     assert X.stride(1) == 1 and Y.stride(1) == 1
@@ -458,9 +475,10 @@ def fs_edge_softmax_workspace_bytes(fmt: FsFormat) -> int:
 def fs_edge_softmax(fmt: FsFormat, vals, out=None, scale: float = 1.0, work=None, stream=None):
     """Row softmax of scale * value over the stored entries, on vals_blk-layout arrays (out may be vals)."""
     if out is None and work is None:
-        got = _calls().softmax(ctypes.addressof(fmt.c), vals, scale, stream, _stream_ptr(stream))
+        got = _calls().softmax(ctypes.addressof(fmt.c), fmt.arena, vals, scale, stream, _stream_ptr(stream))
         if got is not None:
             return _result(got, "fs_edge_softmax")
+    _here(fmt, vals, out, work)
     assert vals.is_cuda and vals.dtype == fmt.torch_dtype and vals.is_contiguous()
     assert vals.numel() == fmt.c.V * fmt.c.nvec
     if out is None:
@@ -478,9 +496,10 @@ def fs_edge_softmax_backward(fmt: FsFormat, probs, grad, out=None, scale: float 
     """Gradient of fs_edge_softmax: scale * p * (g - row sum of p * g), on vals_blk-layout arrays (out may be
     either input)."""
     if out is None and work is None:
-        got = _calls().softmax_backward(ctypes.addressof(fmt.c), probs, grad, scale, stream, _stream_ptr(stream))
+        got = _calls().softmax_backward(ctypes.addressof(fmt.c), fmt.arena, probs, grad, scale, stream, _stream_ptr(stream))
         if got is not None:
             return _result(got, "fs_edge_softmax_backward")
+    _here(fmt, probs, grad, out, work)
     for t in (probs, grad):
         assert t.is_cuda and t.dtype == fmt.torch_dtype and t.is_contiguous() and t.numel() == fmt.c.V * fmt.c.nvec
     if out is None:
@@ -503,6 +522,7 @@ def fs_pack_values(fmt: FsFormat, vals=None, out=None, stream=None):
         raise FsError(rc, "fs_pack_bytes")
     if out is None:
         out = torch.empty(n.value, dtype=torch.uint8, device="cuda")
+    _here(fmt, vals, out)
     if vals is not None:
         assert vals.is_cuda and vals.is_contiguous() and vals.numel() == fmt.c.V * fmt.c.nvec and vals.element_size() == 2
     rc = lib.fs_pack_values(ctypes.byref(fmt.c), vals.data_ptr() if vals is not None else None, out.data_ptr(),
@@ -514,6 +534,7 @@ def fs_pack_values(fmt: FsFormat, vals=None, out=None, stream=None):
 
 def fs_spmm_packed(fmt: FsFormat, packed, B, out=None, work=None, stream=None):
     """C = A @ B with A's values taken from a buffer made by fs_pack_values."""
+    _here(fmt, B, packed, out, work)
     assert B.is_cuda and B.dtype == fmt.torch_dtype and B.dim() == 2 and B.stride(1) == 1 and B.shape[0] == fmt.c.K
     assert packed.is_cuda and packed.dtype == torch.uint8
     N = B.shape[1]
@@ -549,10 +570,11 @@ def fs_attention(fmt: FsFormat, X, Y, H, scale: float = 1.0, out=None, work=None
 
 def _attention_like(name, fmt, X, Y, H, scale, out, work, stream):
     if out is None and work is None:
-        got = _calls().attention(ctypes.addressof(fmt.c), X, Y, H, scale, name == "fs_attention", stream,
+        got = _calls().attention(ctypes.addressof(fmt.c), fmt.arena, X, Y, H, scale, name == "fs_attention", stream,
                                  _stream_ptr(stream))
         if got is not None:
             return _result(got, name)
+    _here(fmt, X, Y, H, out, work)
     for t in (X, Y, H):
         assert t.is_cuda and t.dtype == fmt.torch_dtype and t.dim() == 2 and t.stride(1) == 1
     d, N = X.shape[1], H.shape[1]
@@ -619,9 +641,12 @@ def fs_relative_buckets(buckets: int, max_distance: int, bidirectional: bool = T
     return torch.tensor(of[:0:-1] + [0] + behind, dtype=torch.uint8, device=device)
 
 
-def _beside(like, out, work):
-    """What the caller gave for an output and a workspace lies where the inputs do, the workspace in one piece."""
-    assert (out is None or out.device == like.device) and (work is None or (work.device == like.device and work.is_contiguous()))
+def _beside(fmt, work, *tensors):
+    """Everything lies where the format does, a workspace that the caller gave in one piece; a bias and dropout stand for their tensors."""
+    for t in tensors:
+        _here(fmt, *((t.table, t.buckets) if isinstance(t, FsBucketBias) else (t.state,) if isinstance(t, FsDropout) else (t,)))
+    _here(fmt, work)
+    assert work is None or work.is_contiguous()
 
 
 def _value_heads(fmt, vals):
@@ -634,16 +659,16 @@ def _value_heads(fmt, vals):
 def fs_edge_bias(fmt: FsFormat, vals, bias: FsBucketBias, scale: float = 1.0, out=None, stream=None):
     """scale * value + the bias of the entry, on vals_blk-layout arrays, one or (heads, V*nvec) (out may be vals)."""
     if out is None:
-        got = _calls().edge_bias(ctypes.addressof(fmt.c), vals, bias.table, bias.buckets, bias.shift, scale, _stream_ptr(stream))
+        got = _calls().edge_bias(ctypes.addressof(fmt.c), fmt.arena, vals, bias.table, bias.buckets, bias.shift, scale, _stream_ptr(stream, fmt))
         if got is not None:
             return _result(got, "fs_edge_bias")
     heads = _value_heads(fmt, vals)
-    _beside(vals, out, None)
+    _beside(fmt, None, vals, out, bias)
     if out is None:
         out = torch.empty_like(vals)
     assert out.shape == vals.shape and out.dtype == vals.dtype and out.is_contiguous()
     rc = load_library().fs_edge_bias(ctypes.byref(fmt.c), heads, vals.data_ptr(), float(scale), ctypes.byref(bias._struct(fmt, heads)), out.data_ptr(),
-                                     _stream_ptr(stream))
+                                     _stream_ptr(stream, fmt))
     if rc:
         raise FsError(rc, "fs_edge_bias")
     return out
@@ -661,11 +686,11 @@ def fs_edge_bias_backward(fmt: FsFormat, grad, bias: FsBucketBias, out=None, wor
     """Gradient of the bias table from the gradient of fs_edge_bias's result (the gradient of its values is scale * grad):
     (heads, buckets), or (buckets,) for a single array."""
     if out is None and work is None:
-        got = _calls().edge_bias_backward(ctypes.addressof(fmt.c), grad, bias.table, bias.buckets, bias.shift, stream, _stream_ptr(stream))
+        got = _calls().edge_bias_backward(ctypes.addressof(fmt.c), fmt.arena, grad, bias.table, bias.buckets, bias.shift, stream, _stream_ptr(stream, fmt))
         if got is not None:
             return _result(got, "fs_edge_bias_backward")
     heads = _value_heads(fmt, grad)
-    _beside(grad, out, work)
+    _beside(fmt, work, grad, out, bias)
     n_buckets = bias.table.shape[-1]
     if out is None:
         out = grad.new_empty((heads, n_buckets) if grad.dim() == 2 else (n_buckets,))
@@ -673,7 +698,7 @@ def fs_edge_bias_backward(fmt: FsFormat, grad, bias: FsBucketBias, out=None, wor
     if work is None:
         work = _temporary(max(fs_edge_bias_backward_workspace_bytes(fmt, heads, n_buckets), 16), grad, stream)
     rc = load_library().fs_edge_bias_backward(ctypes.byref(fmt.c), heads, grad.data_ptr(), ctypes.byref(bias._struct(fmt, heads)), out.data_ptr(),
-                                              work.data_ptr(), work.numel() * work.element_size(), _stream_ptr(stream))
+                                              work.data_ptr(), work.numel() * work.element_size(), _stream_ptr(stream, fmt))
     if rc:
         raise FsError(rc, "fs_edge_bias_backward")
     return out
@@ -683,15 +708,15 @@ def fs_edge_dropout(fmt: FsFormat, vals, dropout: FsDropout, out=None, stream=No
     """Dropout on vals_blk-layout arrays, one or (heads, V*nvec): the probabilities in the forward pass, their gradient in the
     backward pass (out may be vals)."""
     if out is None:
-        got = _calls().edge_dropout(ctypes.addressof(fmt.c), vals, dropout.state, dropout.p, _stream_ptr(stream))
+        got = _calls().edge_dropout(ctypes.addressof(fmt.c), fmt.arena, vals, dropout.state, dropout.p, _stream_ptr(stream, fmt))
         if got is not None:
             return _result(got, "fs_edge_dropout")
     heads = _value_heads(fmt, vals)
-    _beside(vals, out, None)
+    _beside(fmt, None, vals, out, dropout)
     if out is None:
         out = torch.empty_like(vals)
     assert out.shape == vals.shape and out.dtype == vals.dtype and out.is_contiguous()
-    rc = load_library().fs_edge_dropout(ctypes.byref(fmt.c), heads, vals.data_ptr(), ctypes.byref(dropout._struct()), out.data_ptr(), _stream_ptr(stream))
+    rc = load_library().fs_edge_dropout(ctypes.byref(fmt.c), heads, vals.data_ptr(), ctypes.byref(dropout._struct()), out.data_ptr(), _stream_ptr(stream, fmt))
     if rc:
         raise FsError(rc, "fs_edge_dropout")
     return out
@@ -726,7 +751,7 @@ def _attention_operands(fmt, X, Y, H, bias, dropout):
     x, heads, d = _head_matrix(X, fmt, fmt.c.M)
     y, kv_heads, dy = _head_matrix(Y, fmt, fmt.c.K)
     h, hv, N = _head_matrix(H, fmt, fmt.c.K)
-    assert dy == d and hv == kv_heads and X.dim() == Y.dim() == H.dim() and X.device == Y.device == H.device
+    assert dy == d and hv == kv_heads and X.dim() == Y.dim() == H.dim()
     return (heads, kv_heads, d, N, x, y, h, None if bias is None else ctypes.byref(bias._struct(fmt, heads)),
             None if dropout is None else ctypes.byref(dropout._struct()))
 
@@ -738,13 +763,13 @@ def fs_attention_forward(fmt: FsFormat, X, Y, H, scale: float = 1.0, bias: Optio
     X: (M, d) or (M, heads, d); Y: (K, d) or (K, kv_heads, d), H the same with N columns; a query head h reads
     keys and values h // (heads // kv_heads).  Returns (out, lse): like X with N columns, and float32 (M,) or (heads, M)."""
     if out is None and lse is None and work is None:
-        got = _calls().attention_forward(ctypes.addressof(fmt.c), X, Y, H, scale, *_bias_args(bias), *_dropout_args(dropout), stream, _stream_ptr(stream))
+        got = _calls().attention_forward(ctypes.addressof(fmt.c), fmt.arena, X, Y, H, scale, *_bias_args(bias), *_dropout_args(dropout), stream,
+                                         _stream_ptr(stream, fmt))
         if got is not None:
             return _result(got, "fs_attention_forward")
     heads, kv_heads, d, N, x, y, h, b, dr = _attention_operands(fmt, X, Y, H, bias, dropout)
     M = fmt.c.M
-    _beside(X, out, work)
-    _beside(X, lse, None)
+    _beside(fmt, work, X, Y, H, out, lse, bias, dropout)
     if out is None:
         out = X.new_empty((M, N) if X.dim() == 2 else (M, heads, N))
     assert out.dim() == X.dim()
@@ -755,7 +780,7 @@ def fs_attention_forward(fmt: FsFormat, X, Y, H, scale: float = 1.0, bias: Optio
     assert lse.is_cuda and lse.dtype == torch.float32 and lse.numel() == heads * M and lse.is_contiguous()
     work, work_ptr, work_bytes = _workspace(fmt, work, X, stream, fs_attention_forward_workspace_bytes, heads, N)
     rc = load_library().fs_attention_forward(ctypes.byref(fmt.c), heads, kv_heads, d, N, float(scale), ctypes.byref(x), ctypes.byref(y), ctypes.byref(h), b, dr,
-                                             ctypes.byref(o), lse.data_ptr(), work_ptr, work_bytes, _stream_ptr(stream))
+                                             ctypes.byref(o), lse.data_ptr(), work_ptr, work_bytes, _stream_ptr(stream, fmt))
     if rc:
         raise FsError(rc, "fs_attention_forward")
     return out, lse
@@ -774,14 +799,13 @@ def fs_attention_backward(fmt: FsFormat, fmt_t: FsFormat, X, Y, H, out, lse, gra
     """The gradients of fs_attention_forward, whose ``out`` and ``lse`` these are, from the gradient ``grad`` of out: (dX, dY, dH,
     dTable), the last None without a bias.  ``fmt_t`` is the format of A^T (fs_csr_transpose, fs_convert)."""
     if dX is None and dY is None and dH is None and dTable is None and work is None:
-        got = _calls().attention_backward(ctypes.addressof(fmt.c), ctypes.addressof(fmt_t.c), X, Y, H, out, lse, grad, scale, *_bias_args(bias),
-                                          *_dropout_args(dropout), stream, _stream_ptr(stream))
+        got = _calls().attention_backward(ctypes.addressof(fmt.c), fmt.arena, ctypes.addressof(fmt_t.c), fmt_t.arena, X, Y, H, out, lse, grad, scale,
+                                          *_bias_args(bias), *_dropout_args(dropout), stream, _stream_ptr(stream, fmt))
         if got is not None:
             return _result(got, "fs_attention_backward")
     heads, kv_heads, d, N, x, y, h, b, dr = _attention_operands(fmt, X, Y, H, bias, dropout)
     M = fmt.c.M
-    for t in (out, lse, grad, dX, dY, dH, dTable):
-        _beside(X, t, work)
+    _beside(fmt, work, fmt_t.arena, X, Y, H, out, lse, grad, dX, dY, dH, dTable, bias, dropout)
     assert out.dim() == grad.dim() == X.dim()
     o, oh, oN = _head_matrix(out, fmt, M)
     g, gh, gN = _head_matrix(grad, fmt, M)
@@ -803,7 +827,7 @@ def fs_attention_backward(fmt: FsFormat, fmt_t: FsFormat, X, Y, H, out, lse, gra
     rc = load_library().fs_attention_backward(
         ctypes.byref(fmt.c), ctypes.byref(fmt_t.c), heads, kv_heads, d, N, float(scale), ctypes.byref(x), ctypes.byref(y), ctypes.byref(h), b, dr,
         ctypes.byref(o), lse.data_ptr(), ctypes.byref(g), *(ctypes.byref(_head_matrix(t, fmt, r)[0]) for t, r in ((dX, M), (dY, fmt.c.K), (dH, fmt.c.K))),
-        None if dTable is None else dTable.data_ptr(), work.data_ptr(), work.numel() * work.element_size(), _stream_ptr(stream))
+        None if dTable is None else dTable.data_ptr(), work.data_ptr(), work.numel() * work.element_size(), _stream_ptr(stream, fmt))
     if rc:
         raise FsError(rc, "fs_attention_backward")
     return dX, dY, dH, dTable
@@ -812,9 +836,10 @@ def fs_attention_backward(fmt: FsFormat, fmt_t: FsFormat, X, Y, H, out, lse, gra
 def fs_blk_to_csr(fmt: FsFormat, blk, out=None, stream=None):
     """Reorder a vals_blk-layout array into CSR order."""
     if out is None:
-        got = _calls().blk_to_csr(ctypes.addressof(fmt.c), blk, _stream_ptr(stream))
+        got = _calls().blk_to_csr(ctypes.addressof(fmt.c), fmt.arena, blk, _stream_ptr(stream))
         if got is not None:
             return _result(got, "fs_blk_to_csr")
+    _here(fmt, blk, out)
     assert _calls().holds16(blk, fmt.c.V * fmt.c.nvec)
     if out is None:
         out = blk.new_empty(fmt.c.nnz)
@@ -828,9 +853,10 @@ def fs_blk_to_csr(fmt: FsFormat, blk, out=None, stream=None):
 def fs_csr_to_blk(fmt: FsFormat, vals_csr, out=None, stream=None):
     """CSR-order values -> vals_blk layout (zeros elsewhere): new values for the same pattern."""
     if out is None:
-        got = _calls().csr_to_blk(ctypes.addressof(fmt.c), vals_csr, _stream_ptr(stream))
+        got = _calls().csr_to_blk(ctypes.addressof(fmt.c), fmt.arena, vals_csr, _stream_ptr(stream))
         if got is not None:
             return _result(got, "fs_csr_to_blk")
+    _here(fmt, vals_csr, out)
     assert vals_csr.is_cuda and vals_csr.dtype == fmt.torch_dtype and vals_csr.is_contiguous()
     assert vals_csr.numel() == fmt.c.nnz
     if out is None:
@@ -847,6 +873,7 @@ def fs_csr_transpose(rowptr, colidx, M: int, K: int, stream=None):
     A's CSR order of entry q of A^T's.  Convert the result with fs_convert for A^T * dC."""
     assert rowptr.is_cuda and colidx.is_cuda and rowptr.dtype == torch.int32 and colidx.dtype == torch.int32
     assert rowptr.is_contiguous() and colidx.is_contiguous() and rowptr.numel() == M + 1
+    assert colidx.device == rowptr.device
     nnz = colidx.numel()
     lib = load_library()
     need = ctypes.c_size_t(0)
@@ -872,6 +899,7 @@ def fs_gather16(src, idx, out=None, stream=None):
         got = _calls().gather16(src, idx, _stream_ptr(stream))
         if got is not None:
             return _result(got, "fs_gather16")
+    assert src.device == idx.device and (out is None or out.device == src.device)
     assert src.is_cuda and idx.is_cuda and idx.dtype == torch.int32 and src.element_size() == 2
     assert src.is_contiguous() and idx.is_contiguous()
     if out is None:

@@ -3,7 +3,7 @@
 // A small product is bound by its host path: the kernel of a 4096-row SpMM takes 4.6 us, its launch 3 us, and marshalling
 // one call in Python 3 us (attention, with more operands, a second launch and a workspace: 7 us).  Here the checks, the
 // allocation of the result and of the workspace and the call are compiled; what is left for Python is to pass the
-// tensors.  Every function takes (address of the fs_format, tensors, ..., stream handle; before it, where a workspace may be
+// tensors.  Every function takes (address of the fs_format, the tensor its arrays lie in, tensors, ..., stream handle; before it, where a workspace may be
 // needed, the stream object or None for the current stream) and returns the result tensor,
 // the library's status as an int where the call failed, or None where an argument is not what the call expects, which
 // the binding's checks in Python then name.
@@ -50,17 +50,25 @@ constexpr Py_ssize_t kEntries = sizeof(Entry) / sizeof(void *);
 const fs_format *format_at(PyObject *o) { return (const fs_format *)PyLong_AsVoidPtr(o); }
 void *pointer(PyObject *o) { return PyLong_AsVoidPtr(o); }
 
-bool of_format(const at::Tensor &t, const fs_format *f)
+// A format and the device its arrays lie on, where every operand of a call has to lie: a pointer does not tell.
+struct Format {
+    const fs_format *c;
+    at::Device home;
+    const fs_format *operator->() const { return c; }
+    operator const fs_format *() const { return c; }
+};
+
+bool of_format(const at::Tensor &t, const Format &f)
 {
-    return t.is_cuda() && t.scalar_type() == (f->dtype == FS_F16 ? at::kHalf : at::kBFloat16);
+    return t.is_cuda() && t.device() == f.home && t.scalar_type() == (f->dtype == FS_F16 ? at::kHalf : at::kBFloat16);
 }
-bool matrix(PyObject *o, const fs_format *f, int64_t rows)
+bool matrix(PyObject *o, const Format &f, int64_t rows)
 {
     if (!THPVariable_Check(o)) return false;
     const at::Tensor &t = THPVariable_Unpack(o);
     return t.dim() == 2 && of_format(t, f) && t.stride(1) == 1 && t.size(0) == rows;
 }
-bool flat(PyObject *o, const fs_format *f, int64_t numel)
+bool flat(PyObject *o, const Format &f, int64_t numel)
 {
     if (!THPVariable_Check(o)) return false;
     const at::Tensor &t = THPVariable_Unpack(o);
@@ -93,7 +101,7 @@ struct Work {
     size_t bytes = 0;
     fs_status st = FS_OK;
     template <typename Query>
-    Work(const fs_format *f, const at::Tensor &like, PyObject *on, Query query)
+    Work(const Format &f, const at::Tensor &like, PyObject *on, Query query)
     {
         if (f->n_split_items == 0) return;
         st = query(&bytes);
@@ -122,10 +130,16 @@ PyObject *bind(PyObject *, PyObject *const *a, Py_ssize_t n)
     PyObject *name(PyObject *, PyObject *const *a, Py_ssize_t n)                                         \
     {                                                                                                    \
         HANDLE_TH_ERRORS                                                                                 \
-        if (n != args) { PyErr_SetString(PyExc_TypeError, "wrong number of arguments"); return nullptr; } \
-        const fs_format *f = format_at(a[0]);                                                            \
-        void *stream = pointer(a[args - 1]);                                                             \
+        if (n != args + 1) {                                                                             \
+            PyErr_SetString(PyExc_TypeError, "wrong number of arguments");                               \
+            return nullptr;                                                                              \
+        }                                                                                                \
+        void *stream = pointer(a[args]);                                                                 \
+        const fs_format *at_ = format_at(a[0]);                                                          \
         if (PyErr_Occurred()) return nullptr;                                                            \
+        if (!THPVariable_Check(a[1])) Py_RETURN_NONE;                                                    \
+        const Format f = {at_, THPVariable_Unpack(a[1]).device()};                                       \
+        a++;                                                                                             \
         fs_status st = FS_OK;
 #define FS_ENTRY_END     \
         END_HANDLE_TH_ERRORS \
@@ -215,14 +229,14 @@ struct Heads {
     fs_head_matrix m;
     int64_t heads = 0, columns = 0;
     bool ok = false;
-    Heads(PyObject *o, const fs_format *f, int64_t rows)
+    Heads(PyObject *o, const Format &f, int64_t rows)
     {
         if (!THPVariable_Check(o)) return;
         const at::Tensor &t = THPVariable_Unpack(o);
         set(t, f, rows);
     }
-    Heads(const at::Tensor &t, const fs_format *f, int64_t rows) { set(t, f, rows); }
-    void set(const at::Tensor &t, const fs_format *f, int64_t rows)
+    Heads(const at::Tensor &t, const Format &f, int64_t rows) { set(t, f, rows); }
+    void set(const at::Tensor &t, const Format &f, int64_t rows)
     {
         const int64_t dim = t.dim();
         if ((dim != 2 && dim != 3) || !of_format(t, f) || t.size(0) != rows || (t.stride(dim - 1) != 1 && rows > 0)) return;
@@ -239,14 +253,14 @@ struct Heads {
 struct Bias {
     fs_bucket_bias b = {};
     bool given = false, ok = true;
-    Bias(PyObject *const *a, const fs_format *f, int64_t heads)
+    Bias(PyObject *const *a, const Format &f, int64_t heads)
     {
         if (a[0] == Py_None) return;
         given = true;
         ok = false;
         if (!THPVariable_Check(a[0]) || !THPVariable_Check(a[1])) return;
         const at::Tensor &t = THPVariable_Unpack(a[0]), &k = THPVariable_Unpack(a[1]);
-        if (!k.is_cuda() || k.scalar_type() != at::kByte || !k.is_contiguous() || k.numel() % 2 != 1 || k.numel() > (1 << 30)) return;
+        if (!k.is_cuda() || k.device() != f.home || k.scalar_type() != at::kByte || !k.is_contiguous() || k.numel() % 2 != 1 || k.numel() > (1 << 30)) return;
         if ((t.dim() != 1 && t.dim() != 2) || !of_format(t, f) || t.stride(-1) != 1 || (t.dim() == 2 ? t.size(0) : 1) != heads) return;
         b.d_table = t.data_ptr();
         b.n_buckets = (int32_t)t.size(-1);
@@ -263,14 +277,14 @@ struct Bias {
 struct Dropout {
     fs_dropout d = {};
     bool given = false, ok = true;
-    explicit Dropout(PyObject *const *a)
+    Dropout(PyObject *const *a, const Format &f)
     {
         if (a[0] == Py_None) return;
         given = true;
         ok = false;
         if (!THPVariable_Check(a[0])) return;
         const at::Tensor &s = THPVariable_Unpack(a[0]);
-        if (!s.is_cuda() || s.scalar_type() != at::kLong || !s.is_contiguous() || s.numel() != 2) return;
+        if (!s.is_cuda() || s.device() != f.home || s.scalar_type() != at::kLong || !s.is_contiguous() || s.numel() != 2) return;
         d.d_state = (const int64_t *)s.data_ptr();
         d.p = PyFloat_AsDouble(a[1]);
         ok = !PyErr_Occurred();
@@ -279,7 +293,7 @@ struct Dropout {
 };
 
 // Value arrays, one or (heads, V * nvec).
-bool value_arrays(PyObject *o, const fs_format *f, int64_t *heads)
+bool value_arrays(PyObject *o, const Format &f, int64_t *heads)
 {
     if (!THPVariable_Check(o)) return false;
     const at::Tensor &t = THPVariable_Unpack(o);
@@ -320,7 +334,7 @@ FS_ENTRY_END
 FS_ENTRY(edge_dropout, 5)  // format, values, state, p, stream
     int64_t heads = 0;
     if (!value_arrays(a[1], f, &heads)) Py_RETURN_NONE;
-    const Dropout drop(a + 2);
+    const Dropout drop(a + 2, f);
     if (PyErr_Occurred()) return nullptr;
     if (!drop.ok || !drop.given) Py_RETURN_NONE;
     const at::Tensor &v = THPVariable_Unpack(a[1]);
@@ -365,7 +379,7 @@ FS_ENTRY(attention_forward, 12)  // format, X, Y, H, scale, table, buckets, shif
     if (!go_together(x, y, h, a + 1) || !stream_or_none(a[10])) Py_RETURN_NONE;
     const float scale = (float)PyFloat_AsDouble(a[4]);
     const Bias bias(a + 5, f, x.heads);
-    const Dropout drop(a + 8);
+    const Dropout drop(a + 8, f);
     if (PyErr_Occurred()) return nullptr;
     if (!bias.ok || !drop.ok) Py_RETURN_NONE;
     const at::Tensor &X = THPVariable_Unpack(a[1]);
@@ -380,21 +394,23 @@ FS_ENTRY(attention_forward, 12)  // format, X, Y, H, scale, table, buckets, shif
     return st == FS_OK ? tuple_of({&out, &lse}) : PyLong_FromLong((long)st);
 FS_ENTRY_END
 
-// format, format of A^T, X, Y, H, out, lse, gradient of out, scale, table, buckets, shift, state, p, stream object, stream
-FS_ENTRY(attention_backward, 16)
+// format, format of A^T, the tensor its arrays lie in, X, Y, H, out, lse, gradient of out, scale, table, buckets, shift, state, p, stream object, stream
+FS_ENTRY(attention_backward, 17)
     const fs_format *ft = format_at(a[1]);
     if (PyErr_Occurred()) return nullptr;
+    if (!THPVariable_Check(a[2]) || THPVariable_Unpack(a[2]).device() != f.home) Py_RETURN_NONE;
+    a++;
     const Heads x(a[2], f, f->M), y(a[3], f, f->K), h(a[4], f, f->K), o(a[5], f, f->M), go(a[7], f, f->M);
     if (!o.ok || !go.ok || !go_together(x, y, h, a + 2) || o.heads != x.heads || go.heads != x.heads || o.columns != h.columns || go.columns != h.columns ||
         !stream_or_none(a[14]) || !THPVariable_Check(a[6]))
         Py_RETURN_NONE;
     const at::Tensor &X = THPVariable_Unpack(a[2]), &Y = THPVariable_Unpack(a[3]), &H = THPVariable_Unpack(a[4]), &lse = THPVariable_Unpack(a[6]);
-    if (THPVariable_Unpack(a[5]).dim() != X.dim() || THPVariable_Unpack(a[7]).dim() != X.dim() || !lse.is_cuda() || lse.scalar_type() != at::kFloat ||
+    if (THPVariable_Unpack(a[5]).dim() != X.dim() || THPVariable_Unpack(a[7]).dim() != X.dim() || !lse.is_cuda() || lse.device() != f.home || lse.scalar_type() != at::kFloat ||
         lse.numel() != x.heads * f->M || !lse.is_contiguous())
         Py_RETURN_NONE;
     const float scale = (float)PyFloat_AsDouble(a[8]);
     const Bias bias(a + 9, f, x.heads);
-    const Dropout drop(a + 12);
+    const Dropout drop(a + 12, f);
     if (PyErr_Occurred()) return nullptr;
     if (!bias.ok || !drop.ok) Py_RETURN_NONE;
     at::Tensor dX = at::empty(X.sizes(), X.options()), dY = at::empty(Y.sizes(), Y.options()), dH = at::empty(H.sizes(), H.options()), dT;
@@ -417,7 +433,7 @@ PyObject *gather16(PyObject *, PyObject *const *a, Py_ssize_t n)  // source, ind
     if (PyErr_Occurred()) return nullptr;
     if (!THPVariable_Check(a[0]) || !THPVariable_Check(a[1])) Py_RETURN_NONE;
     const at::Tensor &src = THPVariable_Unpack(a[0]), &idx = THPVariable_Unpack(a[1]);
-    if (!src.is_cuda() || !idx.is_cuda() || idx.scalar_type() != at::kInt || src.element_size() != 2 || !src.is_contiguous() ||
+    if (!src.is_cuda() || !idx.is_cuda() || src.device() != idx.device() || idx.scalar_type() != at::kInt || src.element_size() != 2 || !src.is_contiguous() ||
         !idx.is_contiguous())
         Py_RETURN_NONE;
     at::Tensor out = at::empty({idx.numel()}, src.options());
