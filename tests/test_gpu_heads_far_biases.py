@@ -120,3 +120,21 @@ def test_rows_whose_scores_are_far_from_zero_without_a_bias(fs, dtype, V, V_t, c
     real = a.ref.scores
     a.ref.scores = lambda h: (real(h)[0], np.zeros_like(s))
     check_gradients(a, l_off=2.0 ** -22 * 4200)
+
+
+@pytest.mark.parametrize("bias", [-LOWEST, LOWEST, -1e30, -1e9, 1e9])
+@pytest.mark.parametrize("V,V_t,chunk,share", SHAPES)
+def test_gradients_agree_with_an_out_that_has_lost_the_scores(fs, bias, V, V_t, chunk, share):  # noqa: F811
+    """fp32 holds nothing of a score of some tens beside such a bias, forward or backward: probabilities that are all equal, in out and in its
+    gradients, whose dS adds up to zero in every row as it has to."""
+    a = far_problem(fs, "bf16", bias, V, V_t, chunk, share)
+    with_operands(a, X=np.random.default_rng(8).standard_normal(a.ref.X.shape))
+    real = a.ref.scores
+
+    def scores(h):
+        s, size = real(h)
+        b = a.ref.table[h][a.ref.bucket]
+        return np.where(a.stored & (np.abs(b) > 1000), b, s), size
+    a.ref.scores = scores
+    check_forward(a)
+    check_gradients(a)
