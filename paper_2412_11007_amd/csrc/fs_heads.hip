@@ -16,12 +16,13 @@
 // (m, l), which k_merge_parts merges in slot order.  l counts what dropout takes out as well: the mask applies after the softmax.
 // Heads are the slower grid dimension, so that one head's rows of Y and H share the L2s; query heads with the same keys are neighbours.
 //
-// Bounds, with 64 columns of both kinds, bias and dropout: on a lognormal graph of 262 k rows, two heads, the fabric (399 us; 2.7 GB fetched,
-// 6.9 of the 7.5 TB/s that such rows reach, since every gathered row misses the L2s); on a sequence of 4096 with a window of 256, eight heads
-// on two, what an entry costs in vector instructions, most of them the generator's, at 58 % of the issue slots (41 us, 2.1 GFLOP); for one row
-// of 1028 entries, eight heads, the chain item -> indices -> rows, 9.8 us.  Wavefronts hide that chain, so registers decide: four a SIMD where
-// tiles of up to 64 columns let them, three up to KS * NT = 16, two above.  Addresses are worked out where they are used, because a spilled
-// one's load waits behind the gathers (four with spills were slower than three without, lognormal graph 458 us and 420).
+// Bounds, with 64 columns of both kinds, bias and dropout: on a lognormal graph of 262 k rows, two heads, the fabric (397 us; 2.7 GB fetched,
+// 6.95 of the 7.5 TB/s that such rows reach, since every gathered row misses the L2s); on a sequence of 4096 with a window of 256, eight heads
+// on two, vector instructions at 58 % of the issue slots, 429 a block of which the generator is 180 (41 us, 2.1 GFLOP); on an R-MAT graph of 65 k
+// rows, 32 and 128 columns, the same at 49 % with two of three wavefronts a SIMD there on average (42 us); for one row of 1028 entries, eight heads,
+// the chain item -> indices -> rows, 10 us.  Wavefronts hide that chain, so registers decide: four a SIMD where tiles of up to 64 columns let
+// them, three up to KS * NT = 16, two above.  Addresses are worked out where they are used, because a spilled one's load waits behind the
+// gathers (four with spills were slower than three without, lognormal graph 458 us and 420).
 #include <type_traits>
 
 #include "fs_common.h"

@@ -22,10 +22,10 @@
 //
 // By columns the query heads that share keys and values are walked inside a block, one after the other, into the same accumulators.
 //
-// Bounds, with 64 columns of both kinds, bias and dropout: on a lognormal graph of 262 k rows, two heads, the fabric (by rows 455 us, 2.9 GB
-// fetched, 6.7 TB/s; by columns 528 us, 3.3 GB, 6.6 TB/s, lines for the 8 bytes {lse, D} of a row among them); on a sequence of 4096
-// with a window of 256, eight heads on two, instructions and too few wavefronts to hide a block's chain (53 and 57 us, 53 % and 40 % of the
-// issue slots; by columns there are two wavefronts a SIMD).  Wavefronts a SIMD: by rows four up to 64 columns, three up to KS * NT = 8; by
+// Bounds, with 64 columns of both kinds, bias and dropout: on a lognormal graph of 262 k rows, two heads, the fabric (by rows 465 us, 2.9 GB
+// fetched, 6.9 TB/s; by columns 546 us, 3.3 GB, 6.7 TB/s, lines for the 8 bytes {lse, D} of a row among them); on a sequence of 4096
+// with a window of 256, eight heads on two, instructions and too few wavefronts to hide a block's chain (53 and 58 us, 51 % and 39 % of the
+// issue slots; by columns 1.3 wavefronts a SIMD on average).  Wavefronts a SIMD: by rows four up to 64 columns, three up to KS * NT = 8; by
 // columns, with two tiles of accumulators and of gathered rows, three up to 64 columns (four spill: 501 us by rows became 562 so, before
 // addresses were worked out where they are used).
 #include <type_traits>
